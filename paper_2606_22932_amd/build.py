@@ -11,9 +11,11 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libforge.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("forge_kernels.hip", "forge_dx.hip", "forge_scratch.hip",
-                                           "forge_api.cpp")]
-HEADERS = [os.path.join(CSRC, "forge_internal.h"), os.path.join(CSRC, "forge_device.h"),
-           os.path.join(INCLUDE, "forge.h")]
+                                           "forge_norm.hip", "forge_multi.hip", "forge_api.cpp",
+                                           "forge_ops_api.cpp")]
+HEADERS = [os.path.join(CSRC, f) for f in ("forge_internal.h", "forge_device.h", "forge_checks.h",
+                                           "forge_ops_internal.h", "forge_ops_device.h")]
+HEADERS += [os.path.join(INCLUDE, f) for f in ("forge.h", "forge_ops.h")]
 
 CEILING_SRC = os.path.join(CSRC, "hbm_ceiling.hip")
 CEILING_BIN = os.path.join(HERE, "hbm_ceiling")   # measured HBM ceilings (bench context)

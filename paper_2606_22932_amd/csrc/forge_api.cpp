@@ -4,31 +4,15 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
-#include <mutex>
 
 #include "forge.h"
+#include "forge_checks.h"
 #include "forge_internal.h"
 
 using forge_impl::Args;
 using forge_impl::Hyper;
 
 namespace {
-
-constexpr int64_t kMaxElems = (int64_t(1) << 31) - 1;
-
-struct Range {
-    uintptr_t lo, hi;   // [lo, hi)
-};
-
-bool overlap(Range a, Range b) { return a.lo < b.hi && b.lo < a.hi; }
-
-Range range_of(const void *p, int64_t bytes)
-{
-    uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-    return Range{lo, lo + static_cast<uintptr_t>(bytes)};
-}
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int64_t moment_bytes(int32_t md) { return md == FORGE_MOMENT_F32 ? 4 : md == FORGE_MOMENT_BF16 ? 2 : 1; }
 
@@ -45,8 +29,6 @@ int64_t scale_bytes(int32_t md, int64_t d_in, int64_t d_out)
     if (md == FORGE_MOMENT_FP8) return 4 * forge_impl::AMAX_SLOTS;
     return ((d_out + 255) / 256) * d_in * 4;
 }
-
-bool finite(float x) { return std::isfinite(x); }
 
 forge_status check_dtype_moment(int32_t md)
 {
@@ -69,16 +51,6 @@ forge_status check_shape(int64_t T, int64_t d_in, int64_t d_out, bool &empty)
     if (d_in * d_out > kMaxElems || T * d_in > kMaxElems || T * d_out > kMaxElems)
         return FORGE_ERR_UNSUPPORTED_SHAPE;
     empty = (d_in == 0 || d_out == 0);
-    return FORGE_OK;
-}
-
-forge_status check_hyper(float lr, float b1, float b2, float eps, float wd, int64_t step)
-{
-    if (step < 1) return FORGE_ERR_INVALID_HYPERPARAM;
-    if (!finite(lr) || !finite(b1) || !finite(b2) || !finite(eps) || !finite(wd))
-        return FORGE_ERR_INVALID_HYPERPARAM;
-    if (!(b1 >= 0.0f && b1 < 1.0f) || !(b2 >= 0.0f && b2 < 1.0f)) return FORGE_ERR_INVALID_HYPERPARAM;
-    if (!(eps > 0.0f) || !(lr >= 0.0f)) return FORGE_ERR_INVALID_HYPERPARAM;
     return FORGE_OK;
 }
 
@@ -153,36 +125,6 @@ forge_status check_inputs(const void *X, const void *dY, int64_t T, int64_t d_in
     (void)d_in;
     (void)d_out;
     return FORGE_OK;
-}
-
-// The current device must be a gfx950; the answer is cached per device ordinal.
-forge_status check_device()
-{
-    static std::mutex mu;
-    static int known[64] = {0};   // 0 unknown, 1 ok, 2 not ok
-    int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0) {
-        (void)hipGetLastError();
-        return FORGE_ERR_NO_DEVICE;
-    }
-    if (dev >= 64) return FORGE_ERR_NO_DEVICE;
-    std::lock_guard<std::mutex> lock(mu);
-    if (known[dev] == 0) {
-        hipDeviceProp_t prop;
-        if (hipGetDeviceProperties(&prop, dev) != hipSuccess) {
-            (void)hipGetLastError();
-            return FORGE_ERR_NO_DEVICE;
-        }
-        known[dev] = (std::strncmp(prop.gcnArchName, "gfx950", 6) == 0) ? 1 : 2;
-    }
-    return known[dev] == 1 ? FORGE_OK : FORGE_ERR_NO_DEVICE;
-}
-
-forge_status from_hip(hipError_t e)
-{
-    if (e == hipSuccess) return FORGE_OK;
-    if (e == hipErrorNoDevice || e == hipErrorInvalidDevice) return FORGE_ERR_NO_DEVICE;
-    return FORGE_ERR_LAUNCH;
 }
 
 Args base_args(const void *X, const void *dY, int64_t T, int64_t d_in, int64_t d_out)

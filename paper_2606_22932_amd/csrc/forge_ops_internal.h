@@ -1,0 +1,86 @@
+// Internal interface between forge_ops_api.cpp and the kernels of forge_norm.hip and
+// forge_multi.hip.  Not installed; callers use include/forge_ops.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace forge_impl {
+
+// ------------------------------------------------------------------------ RMS norm
+
+struct NormArgs {
+    const void *x;         // bf16 [T, d] with a residual, else the stream
+    const void *r;         // residual, or null
+    const void *w;         // [d]
+    void *h;               // the stored sum (with a residual)
+    uint16_t *y;           // bf16 output, or null
+    uint8_t *q;            // fp8 output, or null
+    float *qs;
+    int T, d;
+    int h_bf16, w_bf16;    // element types: bf16 or fp32
+    int q_group;           // columns per scale; 0: the row
+    float eps;
+};
+
+struct NormGradArgs {
+    const uint16_t *dy;
+    const void *h, *w;
+    const void *dres;      // or null
+    void *dh;              // or null
+    uint16_t *dx;          // or null
+    float *dw;
+    float *part;           // [norm_grad_parts(T, d), d]
+    int T, d;
+    int h_bf16, w_bf16;
+    float eps;
+};
+
+hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t stream);
+// T == 0 fills dw with zeros.
+hipError_t launch_rmsnorm_backward(const NormGradArgs &a, hipStream_t stream);
+// Rows of the partial sums of dw: how many workgroups share the T rows.
+inline int norm_grad_parts(int64_t T, int64_t) { return (int)(T < 512 ? T : 512); }
+
+// ------------------------------------------------------------------------ many tensors
+
+// Elements of a chunk, the work of one workgroup's pass; a multiple of the 64 elements that
+// share an fp8 scale.
+constexpr int MT_CHUNK = 2048;
+constexpr int MT_BLOCK = 64;
+// Chunks of a list: a launch has fewer than 2^32 threads.
+constexpr int64_t MT_MAX_CHUNKS = (int64_t(1) << 24) - 1;
+// Workgroups of the gradient norm, each leaving one partial sum.
+constexpr int MT_NORM_PARTS = 2048;
+
+enum MtType { MT_F32 = 0, MT_BF16 = 1, MT_FP8 = 2 };
+
+// A tensor as the kernels read it from the table.
+struct alignas(16) MtTensor {
+    void *W;
+    const void *G;
+    void *m, *v;
+    float *ms, *vs;
+    int32_t numel, first;  // elements; number of its first chunk
+    float lr_scale, wd;
+    int32_t wt, gt, st;    // MtType of weight, gradient, state
+    int32_t pad;
+};
+
+// The table: n tensors, then for each chunk the tensor that it belongs to.
+struct MtTable {
+    const MtTensor *t;
+    const int32_t *owner;
+    int64_t chunks;
+};
+
+struct MtHyper {
+    float b1, c1, b2, c2;  // betas and 1 - betas
+    float inv_sqrt_bc2, eps;
+    double lr, lr_bc1;     // lr, lr / (1 - beta1^t): scaled per tensor, then rounded to fp32
+};
+
+hipError_t launch_grad_norm(const MtTable &t, float max_norm, float *out, double *part, hipStream_t stream);
+hipError_t launch_adamw_multi(const MtTable &t, const MtHyper &h, const float *grad_scale, hipStream_t stream);
+
+}  // namespace forge_impl

@@ -1,4 +1,5 @@
-"""Python binding of the C ABI in ``include/forge.h`` (argument marshalling only).
+"""Python binding of the C ABI in ``include/forge.h`` and ``include/forge_ops.h`` (argument
+marshalling only).
 
 Every function here has the name of the C entry point it calls.  Tensors are torch
 tensors on the current HIP device; their data pointers, shapes and the current torch
@@ -34,6 +35,7 @@ OPTIMIZERS = {"adamw": 0, "sgd": 1, "sgd_momentum": 2, "adagrad": 3, "rmsprop": 
 OPTIMIZER_STATES = {"adamw": 2, "sgd": 0, "sgd_momentum": 1, "adagrad": 1, "rmsprop": 1, "lion": 1, "nadam": 2,
                     "radam": 2, "adamax": 2, "muon_accumulate": 1}
 HEADER = os.path.join(_build.ROOT, "include", "forge.h")
+OPS_HEADER = os.path.join(_build.ROOT, "include", "forge_ops.h")
 
 
 class ForgeError(RuntimeError):
@@ -87,6 +89,32 @@ _SIGS = {
 }
 
 
+class forge_tensor(ctypes.Structure):
+    """``forge_tensor`` of ``include/forge_ops.h``: one tensor of a list."""
+    _fields_ = [("W", _P), ("G", _P), ("m", _P), ("v", _P), ("m_scale", _P), ("v_scale", _P), ("numel", _I64),
+                ("lr_scale", _F), ("weight_decay", _F), ("w_dtype", _I32), ("g_dtype", _I32), ("state_dtype", _I32),
+                ("reserved", _I32)]
+
+
+class forge_tensor_list(ctypes.Structure):
+    """``forge_tensor_list`` of ``include/forge_ops.h``."""
+    _fields_ = [("table_bytes", _I64), ("chunks", _I64), ("n", _I32), ("steppable", _I32)]
+
+
+_LIST = ctypes.POINTER(forge_tensor_list)
+# include/forge_ops.h
+_OPS_SIGS = {
+    "forge_rmsnorm": [_P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I32, _I32, _I32, _F, _P],
+    "forge_rmsnorm_backward": [_P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I32, _I32, _F, _P, _I64, _P],
+    "forge_rmsnorm_backward_workspace": [_I64, _I64],
+    "forge_tensor_list_bytes": [ctypes.POINTER(forge_tensor), _I32],
+    "forge_tensor_list_build": [ctypes.POINTER(forge_tensor), _I32, _P, _I64, _LIST],
+    "forge_grad_norm": [_LIST, _P, _F, _P, _P, _I64, _P],
+    "forge_grad_norm_workspace": [_LIST],
+    "forge_adamw_multi": [_LIST, _P, _F, _F, _F, _F, _P, _I64, _P],
+}
+
+
 def lib():
     """The loaded ``libforge.so`` (raises if it has not been built)."""
     global _lib
@@ -105,9 +133,9 @@ def lib():
     return _lib
 
 
-def header_functions():
-    """Names of the functions ``include/forge.h`` declares."""
-    text = open(HEADER).read()
+def header_functions(path=None):
+    """Names of the functions ``include/forge.h`` (or the header at ``path``) declares."""
+    text = open(path or HEADER).read()
     text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
     return sorted(set(re.findall(r"\b(forge_[a-z_0-9]+)\s*\(", text)))
 
@@ -392,3 +420,240 @@ def forge_linear_step_unfused_noalloc(X, dY, W, m, v, m_scale=None, v_scale=None
                                                  _moment_code(m, m_scale), lr, beta1, beta2, eps, weight_decay,
                                                  int(step), gd, _stream(stream, W))
     _check(st, "forge_linear_step_unfused_noalloc")
+
+
+# ----------------------------------------------------------------------------- include/forge_ops.h
+
+FORGE_DTYPE_F32, FORGE_DTYPE_BF16, FORGE_DTYPE_FP8 = 0, 1, 2
+FORGE_Q_GROUP, FORGE_STATE_BLOCK = 128, 64
+_ops_lib = None
+
+
+def _ops():
+    """``lib()`` with the prototypes of ``include/forge_ops.h``."""
+    global _ops_lib
+    if _ops_lib is None:
+        L = lib()
+        for name, args in _OPS_SIGS.items():
+            fn = getattr(L, name)
+            fn.argtypes = args
+            fn.restype = _I64 if name.endswith(("_workspace", "_bytes")) else _I32
+        _ops_lib = L
+    return _ops_lib
+
+
+def _adr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _float_code(t, what):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return FORGE_DTYPE_BF16
+    if t.dtype == torch.float32:
+        return FORGE_DTYPE_F32
+    raise TypeError(f"{what} must be bfloat16 or float32, got {t.dtype}")
+
+
+def _like(t, what, shape, dtype):
+    if t is not None and (t.shape != shape or t.dtype != dtype):
+        raise ValueError(f"{what} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _bytes_ws(ws, need):
+    if ws is None:
+        if need:
+            raise ValueError(f"ws of {need} bytes needed")
+        return 0
+    if ws.nbytes < need:
+        raise ValueError(f"ws too small: {ws.nbytes} bytes, {need} needed")
+    return ws.nbytes
+
+
+class _on:
+    """The device of ``ref`` made current for a call; every tensor must live there."""
+    __slots__ = ("to", "back")
+
+    def __init__(self, ref, *ts):
+        import torch
+        _dev(ref, *ts)
+        for t in ts:
+            if t is not None and t.device != ref.device:
+                raise ValueError(f"tensors on different devices: {ref.device} and {t.device}")
+        self.to, self.back = ref.device.index, torch.cuda.current_device()
+
+    def __enter__(self):
+        if self.to != self.back:
+            import torch
+            torch.cuda.set_device(self.to)
+
+    def __exit__(self, *exc):
+        if self.to != self.back:
+            import torch
+            torch.cuda.set_device(self.back)
+
+
+def forge_rmsnorm(x, w, *, residual=None, h=None, y=None, q=None, q_scale=None, eps, stream=None):
+    """h = residual + x (rounded to the residual's type), y = h / sqrt(mean(h^2) + eps) * w over
+    the last axis of [T, d] tensors; without a residual y is that of x itself.
+
+    ``y`` is bfloat16; ``q`` float8_e4m3fn with ``q_scale`` float32 [T] (a scale per row) or
+    [T, ceil(d / 128)] (per 128 columns).  ``h`` goes with a residual and may be the residual.
+    """
+    import torch
+    T, d = x.shape
+    with _on(x, w, residual, h, y, q, q_scale):
+        _like(w, "w", (d,), w.dtype)
+        s = x if residual is None else residual
+        if residual is not None:
+            _like(x, "x beside a residual", x.shape, torch.bfloat16)
+            _like(residual, "residual", x.shape, residual.dtype)
+            _like(h, "h", x.shape, residual.dtype)
+        _like(y, "y", x.shape, torch.bfloat16)
+        _like(q, "q", x.shape, torch.float8_e4m3fn)
+        group = 0
+        if q is not None and q_scale is not None:
+            if q_scale.dim() == 2:
+                group = FORGE_Q_GROUP
+            _like(q_scale, "q_scale", (T, (d + 127) // 128) if group else (T,), torch.float32)
+        st = _ops().forge_rmsnorm(_adr(x), _adr(residual), _adr(w), _adr(h), _adr(y), _adr(q), _adr(q_scale), T, d,
+                                  _float_code(s, "the stream"), _float_code(w, "w"), group, eps, _stream(stream, x))
+    _check(st, "forge_rmsnorm")
+
+
+def forge_rmsnorm_backward_workspace(T, d):
+    """Bytes of the workspace of ``forge_rmsnorm_backward`` on [T, d]."""
+    return _ops().forge_rmsnorm_backward_workspace(int(T), int(d))
+
+
+def forge_rmsnorm_backward(dy, h, w, *, dres=None, dh=None, dx=None, dw, eps, ws, stream=None):
+    """The gradient of ``forge_rmsnorm``: dh (in h's type) and / or dx (bfloat16), both
+    dres + the norm's gradient, and dw (float32).  ``h`` is what the norm was taken of; dh may be
+    dres.  ``ws``: any tensor of at least ``forge_rmsnorm_backward_workspace(T, d)`` bytes."""
+    import torch
+    T, d = dy.shape
+    with _on(dy, h, w, dres, dh, dx, dw, ws):
+        _like(dy, "dy", dy.shape, torch.bfloat16)
+        _like(h, "h", dy.shape, h.dtype)
+        _like(w, "w", (d,), w.dtype)
+        _like(dres, "dres", dy.shape, h.dtype)
+        _like(dh, "dh", dy.shape, h.dtype)
+        _like(dx, "dx", dy.shape, torch.bfloat16)
+        _like(dw, "dw", (d,), torch.float32)
+        n = _bytes_ws(ws, forge_rmsnorm_backward_workspace(T, d))
+        st = _ops().forge_rmsnorm_backward(_adr(dy), _adr(h), _adr(w), _adr(dres), _adr(dh), _adr(dx), _adr(dw), T, d,
+                                           _float_code(h, "h"), _float_code(w, "w"), eps, _adr(ws), n,
+                                           _stream(stream, dy))
+    _check(st, "forge_rmsnorm_backward")
+
+
+class TensorList:
+    """Tensors that ``forge_adamw_multi`` steps and ``forge_grad_norm`` reads together.
+
+    ``tensors``: sequence of ``(W, G, m, v)`` or ``(W, G, m, v, m_scale, v_scale)`` tuples of
+    one device, of any shapes and types (W, G float32 or bfloat16; m and v float32, bfloat16, or
+    float8_e4m3fn with float32 scales of ceil(numel / 64) elements); ``(None, G)`` for a list
+    that is only normed.  ``lr_scale`` and ``weight_decay``: a number, or one per tensor.
+
+    Built once for tensors that stay where they are, and held on to while calls or captured
+    graphs use it; it keeps the tensors alive.  Their types are checked and their addresses laid
+    out and copied to the device here, not at each call: after gradients (or anything else) were
+    allocated anew, build another, or give the new ones to ``with_gradients``.
+    """
+
+    def __init__(self, tensors, *, lr_scale=1.0, weight_decay=0.0):
+        import torch
+        self.tensors = [tuple(x) + (None,) * (6 - len(x)) for x in tensors]
+        n = len(self.tensors)
+        each = lambda x: [float(x)] * n if isinstance(x, (int, float)) else [float(y) for y in x]
+        self.lr_scale, self.weight_decay = each(lr_scale), each(weight_decay)
+        if len(self.lr_scale) != n or len(self.weight_decay) != n:
+            raise ValueError("lr_scale and weight_decay: one number, or one per tensor")
+        if any(t[1] is None for t in self.tensors):
+            raise ValueError("a tensor of a list needs its gradient")
+        arr = (forge_tensor * max(n, 1))()
+        self.device = self.tensors[0][1].device if n else None
+        for i, (t, ls, wd) in enumerate(zip(self.tensors, self.lr_scale, self.weight_decay)):
+            arr[i] = self._entry(t, ls, wd)
+        L = _ops()
+        self.list = forge_tensor_list()
+        host = torch.zeros(max(L.forge_tensor_list_bytes(arr, n), 16), dtype=torch.uint8)
+        _check(L.forge_tensor_list_build(arr, n, host.data_ptr(), host.nbytes, ctypes.byref(self.list)), "TensorList")
+        self.table = host.to(self.device) if n else None
+        self._ref = ctypes.byref(self.list)
+        # the table belongs to the stream that is current here (the copy itself has ended)
+        self._home = torch.cuda.current_stream(self.device).cuda_stream if n else 0
+
+    def _entry(self, t, lr_scale, weight_decay):
+        import torch
+        W, G, m, v, ms, vs = t
+        _dev(*(x for x in t if x is not None))
+        if any(x is not None and x.device != self.device for x in t):
+            raise ValueError("the tensors of a list live on one device")
+        e = forge_tensor(G=G.data_ptr(), numel=G.numel(), lr_scale=lr_scale, weight_decay=weight_decay,
+                         g_dtype=_float_code(G, "gradients"))
+        if W is None:
+            return e
+        if m is None or v is None or W.shape != G.shape or m.shape != G.shape or v.shape != G.shape:
+            raise ValueError("W, G, m and v of a tensor have one shape")
+        if m.dtype != v.dtype:
+            raise TypeError(f"m and v have one type, got {m.dtype} and {v.dtype}")
+        e.W, e.m, e.v, e.w_dtype = W.data_ptr(), m.data_ptr(), v.data_ptr(), _float_code(W, "weights")
+        if m.dtype == torch.float8_e4m3fn:
+            for s in (ms, vs):
+                if s is None or s.dtype != torch.float32 or s.numel() != (G.numel() + 63) // 64:
+                    raise ValueError("fp8 moments need float32 scales of ceil(numel / 64) elements")
+            e.m_scale, e.v_scale, e.state_dtype = ms.data_ptr(), vs.data_ptr(), FORGE_DTYPE_FP8
+        else:
+            e.state_dtype = _float_code(m, "moments")
+        return e
+
+    def with_gradients(self, gradients):
+        """A list of the same weights and state with other gradients."""
+        g = list(gradients)
+        if len(g) != len(self.tensors):
+            raise ValueError("one gradient per tensor")
+        return TensorList([(t[0], x) + t[2:] for t, x in zip(self.tensors, g)], lr_scale=self.lr_scale,
+                          weight_decay=self.weight_decay)
+
+    def _use(self, stream):
+        """The stream's handle, the table kept from reuse until that stream is done with it."""
+        import torch
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device).cuda_stream
+        stream = int(stream)
+        if self.table is not None and stream != self._home:
+            self.table.record_stream(torch.cuda.ExternalStream(stream, self.device))
+        return stream
+
+
+def forge_grad_norm_workspace(tensors):
+    """Bytes of the workspace of ``forge_grad_norm`` on a TensorList."""
+    return _ops().forge_grad_norm_workspace(tensors._ref)
+
+
+def forge_grad_norm(tensors, out, *, max_norm, ws, stream=None):
+    """out[0] = the 2-norm of all gradients of a TensorList, out[1] = min(1, max_norm / (out[0] +
+    1e-6)); ``out`` float32 [2], ``out[1:]`` is what ``forge_adamw_multi`` takes as grad_scale."""
+    import torch
+    with _on(out, ws, tensors.table):
+        _like(out, "out", (2,), torch.float32)
+        n = _bytes_ws(ws, forge_grad_norm_workspace(tensors))
+        st = _ops().forge_grad_norm(tensors._ref, _adr(tensors.table), max_norm, _adr(out), _adr(ws), n,
+                                    _stream(stream, out) if tensors.table is None else tensors._use(stream))
+    _check(st, "forge_grad_norm")
+
+
+def forge_adamw_multi(tensors, *, lr, beta1, beta2, eps, step, grad_scale=None, stream=None):
+    """One AdamW step on every tensor of a TensorList in one launch; learning rate and weight
+    decay per tensor as the list says, gradients times ``grad_scale`` (one float32 on the
+    device, read when the step runs)."""
+    import torch
+    if tensors.table is None:
+        return
+    with _on(tensors.table, grad_scale):
+        if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+            raise ValueError("grad_scale must be one float32")
+        st = _ops().forge_adamw_multi(tensors._ref, _adr(tensors.table), lr, beta1, beta2, eps, _adr(grad_scale),
+                                      int(step), tensors._use(stream))
+    _check(st, "forge_adamw_multi")

@@ -1,0 +1,413 @@
+"""forge_grad_norm and forge_adamw_multi against 64 bits (ops_ref.py), forge_adamw and themselves."""
+import pytest
+import torch
+
+import ops_ref as R
+from paper_2606_22932_amd import forge
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+F8 = torch.float8_e4m3fn
+HP = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8)
+
+
+def _say(*a):
+    print(*a, flush=True)
+
+
+def rand(n, std, seed, absolute=False):
+    x = torch.randn(n, generator=torch.Generator().manual_seed(seed)) * std
+    return x.abs() if absolute else x
+
+
+def encode(x, root=False):
+    """Warm fp8 state for a kernel to read: codes and scales of 64 consecutive elements each."""
+    n = x.numel()
+    s, each = R.scales(R.f64(x.sqrt() if root else x).view(1, n), 64)
+    s, each = s[0].float(), s[0].float().repeat_interleave(64)[:n]
+    y = torch.where(each > 0, (x.sqrt() if root else x) / each, torch.zeros_like(x)).clamp(-448, 448)
+    return y.to(F8), s
+
+
+class Tensor:
+    """One tensor of a list on the host, its device copies lying in a guarded buffer of their own."""
+
+    def __init__(self, n, w, g, state, seed, g_std=1e-3, cold=False, shape=None):
+        self.n, self.state = n, state
+        self.shape = shape or (n,)
+        self.host = {"W": rand(n, 0.02, seed).to(DT[w]), "G": rand(n, g_std, seed + 1).to(DT[g])}
+        m, v = rand(n, 1e-4, seed + 2), rand(n, 1e-6, seed + 3, True)
+        if cold:
+            m, v = torch.zeros(n), torch.zeros(n)
+        if state == "fp8":
+            self.host["m"], self.host["ms"] = encode(m)
+            self.host["v"], self.host["vs"] = encode(v, root=True)
+        else:
+            self.host["m"], self.host["v"] = m.to(DT[state]), v.to(DT[state])
+        self.raw, self.dev = {}, {}
+        for k, t in self.host.items():
+            b = t.contiguous().view(torch.uint8)
+            raw = torch.full((b.numel() + 512,), 0xA5, dtype=torch.uint8, device="cuda")
+            raw[256:256 + b.numel()] = b.cuda()
+            self.raw[k] = raw
+            self.dev[k] = raw[256:256 + b.numel()].view(t.dtype).view(t.shape if k in ("ms", "vs") else self.shape)
+
+    def entry(self):
+        return tuple(self.dev.get(k) for k in ("W", "G", "m", "v", "ms", "vs"))
+
+    def after(self):
+        """New values on the host; bytes outside the tensors, and the gradient, must be the old ones."""
+        torch.cuda.synchronize()
+        out = {}
+        for k, t in self.host.items():
+            raw = self.raw[k].cpu()
+            n = raw.numel() - 512
+            assert bool((raw[:256] == 0xA5).all()) and bool((raw[256 + n:] == 0xA5).all()), f"{k} written outside"
+            out[k] = raw[256:256 + n].view(t.dtype)
+        assert torch.equal(out["G"].view(torch.uint8), self.host["G"].view(torch.uint8)), "G changed"
+        return out
+
+    def values(self, of):
+        """m and v as 64-bit values."""
+        if self.state != "fp8":
+            return R.f64(of["m"]), R.f64(of["v"])
+        each = lambda s: R.f64(s).repeat_interleave(64)[:self.n]
+        return R.f64(of["m"].float()) * each(of["ms"]), (R.f64(of["v"].float()) * each(of["vs"])) ** 2
+
+    def check(self, step, lr_scale=1.0, weight_decay=0.0, grad_scale=1.0, hp=HP):
+        old, new = self.host, self.after()
+        m, v = self.values(old)
+        r = R.adamw(R.f64(old["W"]), R.f64(old["G"]), m, v, step=step, lr_scale=lr_scale, weight_decay=weight_decay,
+                    grad_scale=grad_scale, **hp)
+        if self.state == "fp8":                          # decoding: a product with the scale, its square
+            r["em"] = r["em"] + 2 * R.U * m.abs()
+            r["ev"] = r["ev"] + 4 * R.U * v
+        R.stored(new["W"], r["w"], r["ew"], "W")
+        if self.state != "fp8":
+            R.stored(new["m"], r["m"], r["em"], "m")
+            R.stored(new["v"], r["v"], r["ev"], "v")
+            return
+        for k, x, e, floor in (("m", r["m"], r["em"], None), ("v", r["root"], r["er"], r["root"] > 0)):
+            s, _ = R.scales(x.view(1, -1), 64)
+            es, _ = R.scales(e.view(1, -1), 64)
+            R.within(new[k + "s"], s[0], es[0] + 4 * R.U * s[0] + 2 * R.TINY, k + " scales")
+            each = R.f64(new[k + "s"]).repeat_interleave(64)[:self.n]
+            R.coded(new[k], None, each, x, e, k, floor)
+            if floor is not None:
+                assert bool((new[k].float()[floor & (each > 0)] > 0).all()), "a sqrt(v) > 0 stored as zero"
+
+
+KINDS = [(w, g, s) for w in ("bf16", "f32") for g in ("bf16", "f32") for s in ("bf16", "f32", "fp8")]
+SIZES = [1, 2, 7, 8, 9, 63, 64, 65, 100, 511, 2047, 2048, 2049, 4095, 6151, 20000]
+
+
+@pytest.mark.parametrize("w,g,state", KINDS, ids=str)
+def test_adamw_of_every_kind_and_size(w, g, state):
+    _say("adamw", w, g, state)
+    ts = [Tensor(n, w, g, state, seed=10 * n) for n in SIZES]
+    lst = forge.TensorList([t.entry() for t in ts], weight_decay=0.1)
+    forge.forge_adamw_multi(lst, step=10, **HP)
+    for t in ts:
+        t.check(10, weight_decay=0.1)
+
+
+def test_adamw_of_mixed_kinds_scales_and_empty_tensors():
+    """One list of every kind, its own learning-rate factors, decays and an empty tensor, and the
+    clip coefficient from the device; shapes other than one axis."""
+    ts, ls, wd = [], [], []
+    for k, (w, g, s) in enumerate(KINDS + KINDS[::-1]):
+        n = (3 * 37 * (k + 1), 2048, 5, 4099)[k % 4]
+        ts.append(Tensor(n, w, g, s, seed=100 * k, shape=(3, 37, k + 1) if k % 4 == 0 else None))
+        ls.append((1.0, 0.5, 0.0, 2.0)[k % 4])
+        wd.append((0.0, 0.1, -0.05)[k % 3])
+    ts.insert(3, Tensor(0, "bf16", "bf16", "bf16", seed=1))
+    ls.insert(3, 1.0)
+    wd.insert(3, 0.0)
+    coef = torch.tensor([9.0, 0.37], device="cuda")[1:]
+    lst = forge.TensorList([t.entry() for t in ts], lr_scale=ls, weight_decay=wd)
+    forge.forge_adamw_multi(lst, step=3, grad_scale=coef, **HP)
+    for t, a, b in zip(ts, ls, wd):
+        if t.n:
+            t.check(3, lr_scale=a, weight_decay=b, grad_scale=float(coef.cpu()[0]))
+
+
+@pytest.mark.parametrize("state", ["bf16", "f32", "fp8"])
+@pytest.mark.parametrize("step", [1, 100000])
+def test_adamw_cold_and_late(state, step):
+    ts = [Tensor(n, "f32", "f32", state, seed=n, cold=True) for n in (70, 5000)]
+    forge.forge_adamw_multi(forge.TensorList([t.entry() for t in ts]), step=step, **HP)
+    for t in ts:
+        t.check(step)
+
+
+@pytest.mark.parametrize("state", ["bf16", "f32"])
+@pytest.mark.parametrize("g", ["bf16", "f32"])
+def test_bits_of_forge_adamw(state, g):
+    """lr_scale 1 and no grad_scale: bit-identical to the one-tensor call."""
+    ts = [Tensor(r * c, "bf16", g, state, seed=r, shape=(r, c)) for r, c in ((8, 8), (136, 264), (1000, 72))]
+    for t in ts:
+        one = {k: x.clone() for k, x in t.dev.items()}
+        forge.forge_adamw(one["G"], one["W"], one["m"], one["v"], step=7, weight_decay=0.1, **HP)
+        t.one = one
+    forge.forge_adamw_multi(forge.TensorList([t.entry() for t in ts], weight_decay=0.1), step=7, **HP)
+    for t in ts:
+        new = t.after()
+        for k in ("W", "m", "v"):
+            assert torch.equal(new[k].view(torch.uint8), t.one[k].cpu().view(-1).view(torch.uint8)), k
+
+
+@pytest.mark.parametrize("g", ["bf16", "f32"])
+def test_fp8_state_to_the_bit(g):
+    """Codes and scales are those of plain fp32 arithmetic, over several steps that each read the
+    codes of the one before: a last bit lost anywhere would change some of half a million codes."""
+    t = Tensor(500033, "f32", g, "fp8", seed=21)
+    lst = forge.TensorList([t.entry()])
+    coef = torch.tensor([0.37])
+    f = torch.float32
+    one = lambda x: torch.tensor(x, dtype=f)
+    b1, b2 = one(HP["beta1"]), one(HP["beta2"])
+    c1, c2 = one(1 - float(b1)), one(1 - float(b2))
+
+    def code(x, root):
+        n = x.numel()
+        b = torch.nn.functional.pad(x, (0, -n % 64)).view(-1, 64)
+        s = b.abs().amax(-1) * one(1.0 / 448.0)
+        s = torch.where(s < 2.0 ** -126, torch.zeros_like(s), s)
+        q = torch.where(s[:, None] > 0, b / s[:, None], torch.zeros_like(b)).clamp(-448, 448).view(-1)[:n]
+        return (torch.where(x > 0, q.clamp_min(2.0 ** -9), q) if root else q).to(F8), s
+
+    q = {k: t.host[k] for k in ("m", "v", "ms", "vs")}
+    for step in range(2, 6):
+        grad = rand(t.n, 10.0 ** -step, 70 + step).to(DT[g])
+        t.dev["G"].copy_(grad)
+        t.host["G"] = grad
+        forge.forge_adamw_multi(lst, step=step, grad_scale=coef.cuda(), **HP)
+        x = grad.float() * coef
+        each = lambda s: s.repeat_interleave(64)[:t.n]
+        m, v = q["m"].float() * each(q["ms"]), (q["v"].float() * each(q["vs"])).square()
+        m, v = b1 * m + c1 * x, b2 * v + c2 * (x * x)
+        q["m"], q["ms"] = code(m, False)
+        # torch's own fp32 root on the CPU is up to a step off; rounding the fp64 root once more to fp32
+        # is exact (53 >= 2 * 24 + 2 bits)
+        q["v"], q["vs"] = code(v.double().sqrt().float(), True)
+        new = t.after()
+        for k in q:
+            assert torch.equal(new[k].view(torch.uint8), q[k].view(torch.uint8)), (step, k)
+
+
+def test_fp8_state_over_many_steps_stays_near_fp32():
+    """Fifty steps from cold state: each step's codes decode to within their rounding of the state
+    that the step itself computed (checked from the stored state before it, step by step)."""
+    t = Tensor(3001, "f32", "f32", "fp8", seed=5, cold=True)
+    lst = forge.TensorList([t.entry()], weight_decay=0.01)
+    for k in range(1, 51):
+        g = rand(t.n, 10.0 ** -(k % 7), 1000 + k)          # gradients of very different sizes
+        t.host["G"] = g
+        t.dev["G"].copy_(g)
+        forge.forge_adamw_multi(lst, step=k, **HP)
+        t.check(k, weight_decay=0.01)
+        t.host = {n: x.clone() for n, x in t.after().items()}
+
+
+def test_zero_gradients_and_blocks():
+    t = Tensor(200, "f32", "f32", "fp8", seed=3, cold=True)
+    t.dev["G"].zero_()
+    t.host["G"].zero_()
+    forge.forge_adamw_multi(forge.TensorList([t.entry()]), step=1, **HP)
+    new = t.after()
+    assert torch.equal(new["W"], t.host["W"]) and not new["ms"].any() and not new["vs"].any()
+    assert not new["m"].float().any() and not new["v"].float().any()
+
+
+@pytest.mark.parametrize("state", ["bf16", "f32", "fp8"])
+def test_not_finite_gradient(state):
+    """A NaN stays in its element of fp32 and bf16 state, and in its block of 64 of fp8 state."""
+    a, b = (Tensor(300, "f32", "f32", state, seed=9) for _ in range(2))
+    b.dev["G"][130] = float("nan")
+    b.host["G"][130] = float("nan")
+    for t in (a, b):
+        forge.forge_adamw_multi(forge.TensorList([t.entry()]), step=4, **HP)
+    x, y = a.after(), b.after()
+    keep = torch.ones(300, dtype=torch.bool)
+    keep[130] = False
+    assert torch.equal(x["W"][keep], y["W"][keep]) and torch.isnan(y["W"][130])
+    (m0, v0), (m1, v1) = a.values(x), b.values(y)
+    bad = ~keep
+    if state == "fp8":
+        bad[128:192] = True
+    assert torch.equal(m0[~bad], m1[~bad]) and torch.equal(v0[~bad], v1[~bad])
+    assert torch.isnan(m1[bad]).all() and torch.isnan(v1[bad]).all()
+
+
+# ----------------------------------------------------------------------------- gradient norm
+
+def norm_of(grads, max_norm=1.0):
+    dev = [g.cuda() for g in grads]
+    lst = forge.TensorList([(None, g) for g in dev])
+    new = torch.full((4,), 7.0, device="cuda")
+    ws = torch.full((forge.forge_grad_norm_workspace(lst),), 0xFF, dtype=torch.uint8, device="cuda")
+    forge.forge_grad_norm(lst, new[1:3], max_norm=max_norm, ws=ws)
+    out = new.cpu()
+    assert out[0] == 7.0 and out[3] == 7.0
+    return out[1:3]
+
+
+def check_norm(grads, max_norm=1.0):
+    out = R.f64(norm_of(grads, max_norm))
+    n, c = R.grad_norm(grads, max_norm)
+    # sums in 64 bits of at most 2^32 terms: far below the one rounding to fp32, whose largest value
+    # is (2 - 2^-23) 2^127: a norm half a step (2^103) or more above it is rounded to Inf
+    if n >= 2.0 ** 128 - 2.0 ** 103:
+        assert float(out[0]) == float("inf")
+    else:
+        assert abs(float(out[0]) - n) <= 1.01 * R.U * n + 1e-45, (float(out[0]), n)
+    assert abs(float(out[1]) - c) <= 1.01 * R.U * c + 1e-45, (float(out[1]), c)
+
+
+@pytest.mark.parametrize("g", ["bf16", "f32"])
+@pytest.mark.parametrize("sizes", [[1], [8], [65 * 64], [7, 0, 2049, 1, 4096, 63], [3] * 300, [2048 * 2500 + 5], [1 << 20, 9]],
+                         ids=lambda s: str(s[:6]))
+def test_grad_norm(sizes, g):
+    _say("grad_norm", sizes[:8], g)
+    check_norm([rand(n, 1e-3, 5 + k).to(DT[g]) for k, n in enumerate(sizes)])
+
+
+def test_grad_norm_mixed_and_clipping():
+    gs = [rand(1000, 1.0, 1).to(DT["bf16"]), rand(77, 3.0, 2), rand(5000, 1e-3, 3).to(DT["bf16"])]
+    check_norm(gs, max_norm=0.25)
+    check_norm(gs, max_norm=1e4)
+    assert float(norm_of(gs, max_norm=1e4)[1]) == 1.0
+
+
+def test_grad_norm_of_nothing_and_of_zeros():
+    for gs in ([], [torch.zeros(0)], [torch.zeros(4000)]):
+        out = norm_of(gs)
+        assert out.tolist() == [0.0, 1.0]
+
+
+def test_grad_norm_of_extreme_values():
+    """Squares beyond fp32's range on both sides."""
+    check_norm([torch.full((1000,), 1e25), torch.full((5,), 1e-30)])
+    check_norm([torch.full((300,), 1e-30)], max_norm=1e-20)
+    check_norm([torch.full((64,), 3e38).to(DT["bf16"])])  # the norm, 8 times that, is no fp32 number: Inf
+    out = norm_of([torch.full((64,), float("inf")), torch.ones(3)])
+    assert out[0] == float("inf") and out[1] == 0.0
+    out = norm_of([torch.ones(3000), torch.tensor([1.0, float("nan")])])
+    assert torch.isnan(out).all()
+
+
+def test_one_list_normed_and_stepped_in_a_graph():
+    """Norm, then the clipped step, captured once and replayed: each replay equals the eager calls
+    on the same state; two graphs with their own workspaces do not disturb each other."""
+    make = lambda: [Tensor(n, w, g, s, seed=n + 7, g_std=0.1) for n, (w, g, s) in zip((4096, 1000, 33, 70001), KINDS[1::3])]
+    a, b, c = make(), make(), make()
+
+    def plan(ts):
+        lst = forge.TensorList([t.entry() for t in ts], weight_decay=0.1)
+        return lst, torch.zeros(2, device="cuda"), torch.zeros(forge.forge_grad_norm_workspace(lst), dtype=torch.uint8,
+                                                               device="cuda")
+
+    def both(p, step):
+        lst, out, ws = p
+        forge.forge_grad_norm(lst, out, max_norm=1.0, ws=ws)
+        forge.forge_adamw_multi(lst, step=step, grad_scale=out[1:], **HP)
+
+    pa, pb, pc = plan(a), plan(b), plan(c)
+    torch.cuda.synchronize()
+    graphs = []
+    for p in (pa, pb):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            both(p, 5)
+        graphs.append(g)
+    for k in range(3):
+        both(pc, 5)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for x, y, z in zip(a, b, c):
+            z = z.after()
+            for t in (x.after(), y.after()):
+                for n in z:
+                    assert torch.equal(t[n].view(torch.uint8), z[n].view(torch.uint8)), (k, n)
+        assert torch.equal(pa[1], pc[1]) and torch.equal(pb[1], pc[1]) and 0 < float(pc[1][1]) < 1
+
+
+def test_on_another_stream_and_with_new_gradients():
+    a, b = (Tensor(70001, "bf16", "bf16", "bf16", seed=3) for _ in range(2))
+    la = forge.TensorList([a.entry()])
+    lb = forge.TensorList([b.entry()])
+    torch.cuda.synchronize()
+    forge.forge_adamw_multi(la, step=2, **HP)
+    side = torch.cuda.Stream()
+    forge.forge_adamw_multi(lb, step=2, stream=side.cuda_stream, **HP)
+    del lb
+    side.synchronize()
+    x, y = a.after(), b.after()
+    for k in x:
+        assert torch.equal(x[k].view(torch.uint8), y[k].view(torch.uint8)), k
+    # other gradients for the same state: the list with them steps as a list of its own would
+    g = rand(70001, 1e-2, 99).to(torch.bfloat16).cuda()
+    forge.forge_adamw_multi(la.with_gradients([g]), step=3, **HP)
+    forge.forge_adamw_multi(forge.TensorList([(b.dev["W"], g, b.dev["m"], b.dev["v"])]), step=3, **HP)
+    torch.cuda.synchronize()
+    for k in ("W", "m", "v"):
+        assert torch.equal(a.dev[k].view(torch.uint8), b.dev[k].view(torch.uint8)), k
+
+
+def test_large_offsets():
+    """A tensor of more than 2^30 elements: its last elements are stepped, and normed."""
+    n = (1 << 30) + 4099
+    w, g = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    m, v = torch.zeros_like(w), torch.zeros_like(w)
+    g[-3:] = 2.0
+    g[0] = 1.0
+    lst = forge.TensorList([(w, g, m, v)])
+    out = torch.zeros(2, device="cuda")
+    forge.forge_grad_norm(lst, out, max_norm=1.0, ws=torch.empty(forge.forge_grad_norm_workspace(lst), dtype=torch.uint8,
+                                                                 device="cuda"))
+    assert float(out[0]) == pytest.approx(13 ** 0.5, rel=1e-6)
+    forge.forge_adamw_multi(lst, step=1, **{**HP, "lr": 0.5})
+    # mhat / sqrt(vhat) is the gradient's sign in the first step
+    assert torch.allclose(w[-3:].float(), torch.full((3,), -0.5, device="cuda"), rtol=2 ** -7)
+    assert float(w[0]) == pytest.approx(-0.5, rel=2 ** -7) and int(torch.count_nonzero(w)) == 4
+
+
+def test_refusals():
+    w = torch.zeros(64, device="cuda")
+    t = lambda: torch.zeros(64, device="cuda")
+    for bad in ((w, t(), t(), t()[:32]), (w, t()[:32], t(), t()), (w, t(), t(), t().bfloat16()),
+                (w, t(), t().to(F8), t().to(F8)), (w, t(), t(), t().cpu()), (w, t(), None, t()),
+                (w, t(), t().to(F8), t().to(F8), t()[:1], t()[:2])):
+        with pytest.raises((ValueError, TypeError)):
+            forge.TensorList([bad])
+    for bad in ((w.half(), t(), t(), t()), (w, t().half(), t(), t()), (w, t(), t().half(), t().half())):
+        with pytest.raises(TypeError):
+            forge.TensorList([bad])
+    with pytest.raises(ValueError):
+        forge.TensorList([(torch.zeros((8, 8), device="cuda").t(), *(torch.zeros((8, 8), device="cuda") for _ in range(3)))])
+    x = t(), t(), t(), t()
+    for ts, name in (([(w, t(), t(), w)], "FORGE_ERR_ALIASING"), ([x, x], "FORGE_ERR_ALIASING"),
+                     ([(torch.zeros(65, device="cuda")[1:], t(), t(), t())], "FORGE_ERR_MISALIGNED")):
+        with pytest.raises(forge.ForgeError) as e:
+            forge.TensorList(ts)
+        assert e.value.name == name
+    lst = forge.TensorList([(None, t())])
+    with pytest.raises(forge.ForgeError):
+        forge.forge_adamw_multi(lst, step=1, **HP)       # no weight to step
+    out = torch.zeros(2, device="cuda")
+    ws = torch.empty(forge.forge_grad_norm_workspace(lst), dtype=torch.uint8, device="cuda")
+    for k in (dict(out=out[:1]), dict(ws=ws[:-1]), dict(ws=None), dict(out=out.bfloat16())):
+        with pytest.raises(ValueError):
+            forge.forge_grad_norm(**{**dict(tensors=lst, out=out, ws=ws, max_norm=1.0), **k})
+    with pytest.raises(forge.ForgeError):
+        forge.forge_grad_norm(lst, out, ws=ws, max_norm=0.0)
+    full = forge.TensorList([x])
+    for bad in (out, out[:1].double()):
+        with pytest.raises(ValueError):
+            forge.forge_adamw_multi(full, step=1, grad_scale=bad, **HP)
+    torch.cuda.synchronize()
