@@ -14,7 +14,7 @@ static_assert(MT_CHUNK == NTH * 8, "a thread's share of a chunk is eight element
 template <int TY> __device__ __forceinline__ void load_some(const void *p, size_t i, int n, float (&f)[8])
 {
     if (n >= 8) {
-        load8<TY == MT_BF16>(p, i, f);
+        load_n<TY == MT_BF16>(p, i, f);
         return;
     }
 #pragma unroll
@@ -29,7 +29,7 @@ template <int TY> __device__ __forceinline__ void load_some(const void *p, size_
 template <int TY> __device__ __forceinline__ void store_some(void *p, size_t i, int n, const float (&f)[8])
 {
     if (n >= 8) {
-        store8<TY == MT_BF16>(p, i, f);
+        store_n<TY == MT_BF16>(p, i, f);
         return;
     }
 #pragma unroll
@@ -120,8 +120,8 @@ __device__ __forceinline__ void adamw_chunk(const MtTensor &t, size_t i, int n, 
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             if (k >= n) m[k] = root[k] = 0.0f;
-        const float ms = e4m3_scale(lanes_max<8>(mag8(m)));
-        const float vs = e4m3_scale(lanes_max<8>(mag8(root)));
+        const float ms = e4m3_scale(lanes_max(mag_n(m), 8));
+        const float vs = e4m3_scale(lanes_max(mag_n(root), 8));
         float lo[8];
         if (n > 0 && i % MT_BLOCK == 0) {
             t.ms[i / MT_BLOCK] = ms;
@@ -133,8 +133,9 @@ __device__ __forceinline__ void adamw_chunk(const MtTensor &t, size_t i, int n, 
             lo[k] = root[k] > 0.0f ? 0x1p-9f : 0.0f;      // a sqrt(v) > 0 is not stored as zero
             root[k] = vs > 0.0f ? root[k] / vs : 0.0f;
         }
-        store_codes(t.m, i, n, e4m3_encode8(m));
-        store_codes(t.v, i, n, e4m3_encode8(root, lo));
+        store_codes(t.m, i, n, u32x2_t{e4m3_encode4(m[0], m[1], m[2], m[3]), e4m3_encode4(m[4], m[5], m[6], m[7])});
+        store_codes(t.v, i, n, u32x2_t{e4m3_encode4(root[0], root[1], root[2], root[3], lo[0], lo[1], lo[2], lo[3]),
+                                e4m3_encode4(root[4], root[5], root[6], root[7], lo[4], lo[5], lo[6], lo[7])});
     } else {
         store_some<ST>(t.m, i, n, m);
         store_some<ST>(t.v, i, n, v);

@@ -1,88 +1,372 @@
 // forge_norm.hip -- residual add and RMS norm, forward and backward (include/forge_ops.h).
+//
+// A row stays in registers between the sum of squares and the outputs, so every input is read
+// once and every output written once.  A row belongs to WR waves: one for up to 4096 columns,
+// whose reductions are lane exchanges and need no barrier; several for wider rows, which join
+// through LDS.  Narrow rows share a wave, 8, 16, 32 or 64 lanes each.
 #include "forge_ops_device.h"
 #include "forge_ops_internal.h"
+
+#include <type_traits>
 
 namespace forge_impl {
 
 namespace {
 
-constexpr int NTH = 256;
-constexpr int MAX_GROUPS = 1 << 20;
+// A thread's part of a row: E elements in vectors of V, the vectors of a row dealt out to its
+// lanes in turn, so that each access of a wave is one dense run.  V is what makes every type's
+// access dense at 16 bytes at most: 8 with a bf16 stream, 4 with an fp32 one.
+template <bool HB, int E, int WR> struct Row {
+    static constexpr int V = HB ? 8 : 4, NV = E / V;
+    int lane, lanes;       // of this row: the thread's place and how many there are
+    int slot, slots;       // the row's place among those that the workgroup holds at once
+    int nv;                // vectors of a row
 
-// One workgroup per row, the row read once for the sum of squares and once more (from cache)
-// for the outputs.
-template <bool HB, bool WB>
-__global__ void __launch_bounds__(NTH) norm_kernel(NormArgs a)
+    __device__ __forceinline__ Row(int d)
+    {
+        nv = d / V;
+        lanes = 64 * WR;
+        if (WR == 1)
+            while (lanes > 8 && lanes * E >= 2 * d) lanes >>= 1;
+        lane = threadIdx.x & (lanes - 1);
+        slot = threadIdx.x / lanes;
+        slots = blockDim.x / lanes;
+    }
+    __device__ __forceinline__ int vec(int j) const { return j * lanes + lane; }
+    __device__ __forceinline__ bool has(int j) const { return vec(j) < nv; }
+};
+
+// Sums over a row: lane exchanges, and for rows of several waves one trip through LDS.  `red`
+// holds 2 * 2 * 16 values, used in turn by rows of even and odd `turn`, so that one barrier a
+// row is enough.
+template <int WR, int N, class R>
+__device__ __forceinline__ void row_sum(float (&x)[N], const R &row, float (*red)[2][16], int turn)
 {
-    __shared__ float red[NTH / 64];
-    __shared__ uint32_t redm[NTH / 64];
-    const int nv = a.d >> 3;
-    const void *src = a.r ? a.h : a.x;
-    for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
-    const size_t row = (size_t)t * a.d;
-    __syncthreads();                                      // red and redm are free
-    float sum = 0.0f;
-    for (int v = threadIdx.x; v < nv; v += NTH) {
-        const size_t i = row + 8 * v;
-        float f[8];
-        if (a.r) {
-            float x[8];
-            load8<true>(a.x, i, x);
-            load8<HB>(a.r, i, f);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = as_stored<HB>(f[k] + x[k]);
-            store8<HB>(a.h, i, f);
-        } else {
-            load8<HB>(a.x, i, f);
-        }
+    for (int k = 0; k < N; ++k) x[k] = lanes_sum(x[k], WR == 1 ? row.lanes : 64);
+    if constexpr (WR > 1) {
+        if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum = __builtin_fmaf(f[k], f[k], sum);
-    }
-    sum = group_sum<NTH>(sum, red);
-    const float s = __builtin_amdgcn_rsqf(sum / a.d + a.eps);
-    auto out8 = [&](int v, float (&f)[8]) {
-        float w[8];
-        load8<HB>(src, row + 8 * v, f);
-        load8<WB>(a.w, 8 * v, w);
+            for (int k = 0; k < N; ++k) red[turn & 1][k][threadIdx.x >> 6] = x[k];
+        }
+        lds_barrier();
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = f[k] * s * w[k];
-    };
-    float rs = 0.0f, rinv = 0.0f;
-    if (a.q && a.q_group == 0) {
-        uint32_t b = 0;
-        for (int v = threadIdx.x; v < nv; v += NTH) {
-            float f[8];
-            out8(v, f);
-            b = max(b, mag8(f));
-        }
-        rs = e4m3_scale(group_max<NTH>(b, redm));
-        rinv = e4m3_inverse(rs);
-        if (threadIdx.x == 0) a.qs[t] = rs;
-    }
-    const int groups = (nv + 15) >> 4;
-    for (int v = threadIdx.x; v < (nv + 63) / 64 * 64; v += NTH) {     // whole waves
-        float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (v < nv) out8(v, f);
-        if (a.q && a.q_group) {
-            rs = e4m3_scale(lanes_max<16>(mag8(f)));
-            rinv = e4m3_inverse(rs);
-            if (v < nv && (v & 15) == 0) a.qs[(size_t)t * groups + (v >> 4)] = rs;
-        }
-        if (v >= nv) continue;
-        if (a.y) store8<true>(a.y, row + 8 * v, f);
-        if (a.q) {
+        for (int k = 0; k < N; ++k) {
+            x[k] = 0.0f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] *= rinv;
-            *reinterpret_cast<u32x2_t *>(a.q + row + 8 * v) = e4m3_encode8(f);
+            for (int i = 0; i < WR; ++i) x[k] += red[turn & 1][k][row.slot * WR + i];
         }
-    }
     }
 }
 
-// Workgroup b takes rows b, b + parts, ...: dh and dx of each, and its share of dw, which it
-// sums in its row of the workspace.
+template <bool HB, bool WB, int E, int WR>
+__global__ void __launch_bounds__(WR == 1 ? 256 : 64 * WR) norm_kernel(NormArgs a)
+{
+    using R = Row<HB, E, WR>;
+    constexpr int V = R::V, NV = R::NV;
+    __shared__ float red[2][2][16];
+    __shared__ uint32_t redm[2][16];
+    const R row(a.d);
+    const float inv_d = 1.0f / a.d;
+    const int stride = gridDim.x * row.slots, groups = (a.d + 127) >> 7;
+    // every wave runs as many turns as the first, rows past the end empty: lane exchanges and
+    // barriers need all of them
+    int turn = 0;
+    for (int t0 = blockIdx.x * row.slots; t0 < a.T; t0 += stride, ++turn) {
+        const int t = t0 + row.slot;
+        const bool live = t < a.T;
+        const size_t at = (size_t)t * a.d;
+        float f[NV][V], sum[1] = {0.0f};
+        {
+            Raw<HB, V> r[NV];
+            if (a.r) {
+                Raw<true, V> x[NV];
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    x[j].zero();
+                    r[j].zero();
+                    if (live && row.has(j)) {
+                        x[j].load(a.x, at + V * row.vec(j));
+                        r[j].load(a.r, at + V * row.vec(j));
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) f[j][k] = r[j].at(k) + x[j].at(k);
+                    r[j].set(f[j]);
+                    if (live && row.has(j)) r[j].store(a.h, at + V * row.vec(j));
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    r[j].zero();
+                    if (live && row.has(j)) r[j].load(a.x, at + V * row.vec(j));
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    f[j][k] = r[j].at(k);                      // the sum as it is stored
+                    sum[0] = __builtin_fmaf(f[j][k], f[j][k], sum[0]);
+                }
+        }
+        row_sum<WR, 1>(sum, row, red, turn);
+        const float s = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[0], inv_d, a.eps));
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (!row.has(j)) continue;
+            float w[V];
+            load_n<WB>(a.w, V * row.vec(j), w);
+#pragma unroll
+            for (int k = 0; k < V; ++k) f[j][k] = f[j][k] * s * w[k];
+            if (live && a.y) store_n<true>(a.y, at + V * row.vec(j), f[j]);
+            top = max(top, mag_n(f[j]));
+        }
+        if (!a.q) continue;
+        float qs = 0.0f, inv = 0.0f;
+        if (a.q_group == 0) {
+            top = lanes_max(top, WR == 1 ? row.lanes : 64);
+            if constexpr (WR > 1) {
+                if ((threadIdx.x & 63) == 0) redm[turn & 1][threadIdx.x >> 6] = top;
+                lds_barrier();
+#pragma unroll
+                for (int i = 0; i < WR; ++i) top = max(top, redm[turn & 1][i]);
+            }
+            qs = e4m3_scale(top);
+            inv = e4m3_inverse(qs);
+            if (live && row.lane == 0) a.qs[t] = qs;
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (a.q_group) {
+                // 128 columns are 128 / V lanes (the launcher gives a row of up to 128 one scale)
+                qs = e4m3_scale(lanes_max(row.has(j) ? mag_n(f[j]) : 0u, 128 / V));
+                inv = e4m3_inverse(qs);
+                if (live && row.has(j) && row.vec(j) % (128 / V) == 0)
+                    a.qs[(size_t)t * groups + row.vec(j) / (128 / V)] = qs;
+            }
+            if (!live || !row.has(j)) continue;
+            uint32_t *q = reinterpret_cast<uint32_t *>(a.q + at + V * row.vec(j));
+            if constexpr (V == 8) {
+                const u32x2_t c = {e4m3_encode4(f[j][0] * inv, f[j][1] * inv, f[j][2] * inv, f[j][3] * inv),
+                                   e4m3_encode4(f[j][4] * inv, f[j][5] * inv, f[j][6] * inv, f[j][7] * inv)};
+                *reinterpret_cast<u32x2_t *>(q) = c;
+            } else {
+                *q = e4m3_encode4(f[j][0] * inv, f[j][1] * inv, f[j][2] * inv, f[j][3] * inv);
+            }
+        }
+    }
+}
+
+// Each workgroup takes its rows in turn: dh and dx of each, and their share of dw in registers,
+// which it leaves in its row of the workspace.  The next rows are loaded ahead of the sums of
+// these, so that loads are in flight across the barrier.
+template <bool HB, int E, int WR> struct GradRow {
+    static constexpr int V = Row<HB, E, WR>::V, NV = Row<HB, E, WR>::NV;
+    Raw<HB, V> h[NV], o[NV];
+    Raw<true, V> g[NV];
+    __device__ __forceinline__ void load(const NormGradArgs &a, const Row<HB, E, WR> &row, int t)
+    {
+        const size_t at = (size_t)t * a.d;
+        const bool live = t < a.T;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            h[j].zero();
+            g[j].zero();
+            o[j].zero();
+            if (!live || !row.has(j)) continue;
+            h[j].load(a.h, at + V * row.vec(j));
+            g[j].load(a.dy, at + V * row.vec(j));
+            if (a.dres) o[j].load(a.dres, at + V * row.vec(j));
+        }
+    }
+};
+
+template <bool HB, bool WB, int E, int WR>
+__global__ void __launch_bounds__(WR == 16 ? 1024 : 512) norm_grad_kernel(NormGradArgs a)
+{
+    using R = Row<HB, E, WR>;
+    constexpr int V = R::V, NV = R::NV;
+    __shared__ float red[2][2][16];
+    __shared__ float share[WR == 16 ? 1 : 64 * WR * E];
+    const R row(a.d);
+    const float inv_d = 1.0f / a.d;
+    const int stride = gridDim.x * row.slots;
+    float acc[NV][V];
+    Raw<WB, V> w[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        w[j].zero();
+        if (row.has(j)) w[j].load(a.w, V * row.vec(j));
+#pragma unroll
+        for (int k = 0; k < V; ++k) acc[j][k] = 0.0f;
+    }
+    GradRow<HB, E, WR> now, next;
+    now.load(a, row, blockIdx.x * row.slots + row.slot);
+    int turn = 0;
+    for (int t0 = blockIdx.x * row.slots; t0 < a.T; t0 += stride, ++turn) {
+        const int t = t0 + row.slot;
+        const size_t at = (size_t)t * a.d;
+        next.load(a, row, t < a.T - stride ? t + stride : a.T);
+        float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                sum[0] = __builtin_fmaf(now.h[j].at(k), now.h[j].at(k), sum[0]);
+                sum[1] = __builtin_fmaf(now.g[j].at(k) * w[j].at(k), now.h[j].at(k), sum[1]);
+            }
+        row_sum<WR, 2>(sum, row, red, turn);
+        const float s = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[0], inv_d, a.eps));
+        const float c = s * s * (sum[1] * inv_d);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float x[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                x[k] = __builtin_fmaf(s, __builtin_fmaf(-now.h[j].at(k), c, now.g[j].at(k) * w[j].at(k)), now.o[j].at(k));
+                acc[j][k] = __builtin_fmaf(now.g[j].at(k), now.h[j].at(k) * s, acc[j][k]);
+            }
+            if (t >= a.T || !row.has(j)) continue;
+            if (a.dh) store_n<HB>(a.dh, at + V * row.vec(j), x);
+            if (a.dx) store_n<true>(a.dx, at + V * row.vec(j), x);
+        }
+        now = next;
+    }
+    float *part = a.part + (size_t)blockIdx.x * a.d;
+    if constexpr (WR < 16) {
+        // the rows that the workgroup held at once, one after the other
+        for (int i = 0; i < row.slots; ++i) {
+            if (row.slot == i) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    if (!row.has(j)) continue;
+                    if (i) {
+                        float x[V];
+                        load_n<false>(share, V * row.vec(j), x);
+#pragma unroll
+                        for (int k = 0; k < V; ++k) acc[j][k] += x[k];
+                    }
+                    if (i + 1 < row.slots) store_n<false>(share, V * row.vec(j), acc[j]);
+                    else store_n<false>(part, V * row.vec(j), acc[j]);
+                }
+            }
+            lds_barrier();
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (row.has(j)) store_n<false>(part, V * row.vec(j), acc[j]);
+    }
+}
+
+// dw: the parts' sum.  A workgroup takes 64 columns, 16 threads of four columns by 16 runs of
+// parts, joined through LDS in the runs' order.
+__global__ void __launch_bounds__(256) norm_dw_kernel(const float *part, float *dw, int parts, int d)
+{
+    __shared__ f32x4_t red[16][16];
+    const int c = threadIdx.x & 15, r = threadIdx.x >> 4, j = (blockIdx.x * 16 + c) * 4;
+    f32x4_t x = {0, 0, 0, 0};
+    if (j < d)
+        for (int p = r; p < parts; p += 16) x += *reinterpret_cast<const f32x4_t *>(part + (size_t)p * d + j);
+    red[r][c] = x;
+    __syncthreads();
+    if (r || j >= d) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) x += red[k][c];
+    *reinterpret_cast<f32x4_t *>(dw + j) = x;
+}
+
+// Rows wider than registers hold: the row is read again (from cache) for the outputs.
+constexpr int NTH = 256;
+
+__device__ __forceinline__ float wide_sum(float x, float *red)
+{
+    x = lanes_sum(x, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NTH / 64; ++k) x += red[k];
+    return x;
+}
+
 template <bool HB, bool WB>
-__global__ void __launch_bounds__(NTH) norm_grad_kernel(NormGradArgs a)
+__global__ void __launch_bounds__(NTH) norm_wide_kernel(NormArgs a)
+{
+    __shared__ float red[NTH / 64];
+    __shared__ uint32_t redm[NTH / 64];
+    const int nv = a.d >> 3, groups = (a.d + 127) >> 7;
+    const void *src = a.r ? a.h : a.x;
+    for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
+        const size_t row = (size_t)t * a.d;
+        __syncthreads();                                      // red and redm are free
+        float sum = 0.0f;
+        for (int v = threadIdx.x; v < nv; v += NTH) {
+            const size_t i = row + 8 * v;
+            float f[8];
+            if (a.r) {
+                float x[8];
+                load_n<true>(a.x, i, x);
+                load_n<HB>(a.r, i, f);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) f[k] = as_stored<HB>(f[k] + x[k]);
+                store_n<HB>(a.h, i, f);
+            } else {
+                load_n<HB>(a.x, i, f);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum = __builtin_fmaf(f[k], f[k], sum);
+        }
+        const float s = __builtin_amdgcn_rsqf(wide_sum(sum, red) / a.d + a.eps);
+        auto out8 = [&](int v, float (&f)[8]) {
+            float w[8];
+            load_n<HB>(src, row + 8 * v, f);
+            load_n<WB>(a.w, 8 * v, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = f[k] * s * w[k];
+        };
+        float qs = 0.0f, inv = 0.0f;
+        if (a.q && a.q_group == 0) {
+            uint32_t top = 0;
+            for (int v = threadIdx.x; v < nv; v += NTH) {
+                float f[8];
+                out8(v, f);
+                top = max(top, mag_n(f));
+            }
+            top = lanes_max(top, 64);
+            if ((threadIdx.x & 63) == 0) redm[threadIdx.x >> 6] = top;
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < NTH / 64; ++k) top = max(top, redm[k]);
+            qs = e4m3_scale(top);
+            inv = e4m3_inverse(qs);
+            if (threadIdx.x == 0) a.qs[t] = qs;
+        }
+        for (int v = threadIdx.x; v < (nv + 63) / 64 * 64; v += NTH) {     // whole waves
+            float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (v < nv) out8(v, f);
+            if (a.q && a.q_group) {
+                qs = e4m3_scale(lanes_max(mag_n(f), 16));
+                inv = e4m3_inverse(qs);
+                if (v < nv && (v & 15) == 0) a.qs[(size_t)t * groups + (v >> 4)] = qs;
+            }
+            if (v >= nv) continue;
+            if (a.y) store_n<true>(a.y, row + 8 * v, f);
+            if (a.q) {
+                const u32x2_t c = {e4m3_encode4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
+                                   e4m3_encode4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)};
+                *reinterpret_cast<u32x2_t *>(a.q + row + 8 * v) = c;
+            }
+        }
+    }
+}
+
+template <bool HB, bool WB>
+__global__ void __launch_bounds__(NTH) norm_grad_wide_kernel(NormGradArgs a)
 {
     __shared__ float red[2][NTH / 64];
     const int nv = a.d >> 3;
@@ -91,9 +375,9 @@ __global__ void __launch_bounds__(NTH) norm_grad_kernel(NormGradArgs a)
         const size_t row = (size_t)t * a.d;
         float s1 = 0.0f, s2 = 0.0f;
         auto in8 = [&](int v, float (&h)[8], float (&g)[8], float (&w)[8]) {
-            load8<HB>(a.h, row + 8 * v, h);
-            load8<true>(a.dy, row + 8 * v, g);
-            load8<WB>(a.w, 8 * v, w);
+            load_n<HB>(a.h, row + 8 * v, h);
+            load_n<true>(a.dy, row + 8 * v, g);
+            load_n<WB>(a.w, 8 * v, w);
         };
         for (int v = threadIdx.x; v < nv; v += NTH) {
             float h[8], g[8], w[8];
@@ -105,58 +389,96 @@ __global__ void __launch_bounds__(NTH) norm_grad_kernel(NormGradArgs a)
             }
         }
         __syncthreads();                                  // red is free
-        s1 = group_sum<NTH>(s1, red[0]);
-        s2 = group_sum<NTH>(s2, red[1]);
+        s1 = wide_sum(s1, red[0]);
+        s2 = wide_sum(s2, red[1]);
         const float s = __builtin_amdgcn_rsqf(s1 / a.d + a.eps);
         const float c = s * s * (s2 / a.d);
         for (int v = threadIdx.x; v < nv; v += NTH) {
             float h[8], g[8], w[8], o[8] = {0, 0, 0, 0, 0, 0, 0, 0}, p[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             in8(v, h, g, w);
-            if (a.dres) load8<HB>(a.dres, row + 8 * v, o);
-            if (!first) load8<false>(part, 8 * v, p);
+            if (a.dres) load_n<HB>(a.dres, row + 8 * v, o);
+            if (!first) load_n<false>(part, 8 * v, p);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 o[k] = __builtin_fmaf(s, __builtin_fmaf(-h[k], c, g[k] * w[k]), o[k]);
                 p[k] = __builtin_fmaf(g[k], h[k] * s, p[k]);
             }
-            if (a.dh) store8<HB>(a.dh, row + 8 * v, o);
-            if (a.dx) store8<true>(a.dx, row + 8 * v, o);
-            store8<false>(part, 8 * v, p);
+            if (a.dh) store_n<HB>(a.dh, row + 8 * v, o);
+            if (a.dx) store_n<true>(a.dx, row + 8 * v, o);
+            store_n<false>(part, 8 * v, p);
         }
     }
 }
 
-// dw: the parts' sum, column by column.
-__global__ void __launch_bounds__(64) norm_dw_kernel(const float *part, float *dw, int parts, int d)
+template <int N> using Int = std::integral_constant<int, N>;
+
+// f(E, WR): the elements that a thread holds of a row of d columns and the waves of the row.
+template <class F> void norm_width(int64_t d, F f)
 {
-    const int j = blockIdx.x * 64 + threadIdx.x;
-    if (j >= d) return;
-    float x = 0.0f;
-    for (int p = 0; p < parts; ++p) x += part[(size_t)p * d + j];
-    dw[j] = x;
+    if (d <= 512) f(Int<8>(), Int<1>());
+    else if (d <= 1024) f(Int<16>(), Int<1>());
+    else if (d <= 2048) f(Int<32>(), Int<1>());
+    else if (d <= 4096) f(Int<64>(), Int<1>());
+    else if (d <= 8192) f(Int<32>(), Int<4>());
+    else if (d <= 16384) f(Int<64>(), Int<4>());
+    else f(Int<32>(), Int<16>());
+}
+template <class F> void grad_width(int64_t d, F f)
+{
+    if (d <= 512) f(Int<8>(), Int<1>());
+    else if (d <= 1024) f(Int<16>(), Int<1>());
+    else if (d <= 2048) f(Int<16>(), Int<2>());
+    else if (d <= 4096) f(Int<16>(), Int<4>());
+    else if (d <= 8192) f(Int<16>(), Int<8>());
+    else f(Int<16>(), Int<16>());
+}
+
+template <bool HB, bool WB> void run_norm(const NormArgs &a, hipStream_t stream)
+{
+    if (a.d > NORM_WIDEST) {
+        norm_wide_kernel<HB, WB><<<min(a.T, 1 << 20), NTH, 0, stream>>>(a);
+        return;
+    }
+    norm_width(a.d, [&](auto e, auto wr) {
+        constexpr int E = decltype(e)::value, WR = decltype(wr)::value;
+        const NormPlan p = norm_plan(a.T, a.d);
+        norm_kernel<HB, WB, E, WR><<<p.groups, p.threads, 0, stream>>>(a);
+    });
+}
+
+template <bool HB, bool WB> void run_grad(const NormGradArgs &a, int parts, hipStream_t stream)
+{
+    if (a.d > GRAD_WIDEST) {
+        norm_grad_wide_kernel<HB, WB><<<parts, NTH, 0, stream>>>(a);
+        return;
+    }
+    grad_width(a.d, [&](auto e, auto wr) {
+        constexpr int E = decltype(e)::value, WR = decltype(wr)::value;
+        norm_grad_kernel<HB, WB, E, WR><<<parts, norm_grad_plan(a.T, a.d).threads, 0, stream>>>(a);
+    });
 }
 
 }  // namespace
 
-hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t stream)
+hipError_t launch_rmsnorm(const NormArgs &args, hipStream_t stream)
 {
-    auto k = a.h_bf16 ? (a.w_bf16 ? norm_kernel<true, true> : norm_kernel<true, false>)
-                      : (a.w_bf16 ? norm_kernel<false, true> : norm_kernel<false, false>);
-    k<<<a.T < MAX_GROUPS ? a.T : MAX_GROUPS, NTH, 0, stream>>>(a);
+    NormArgs a = args;
+    if (a.d <= 128) a.q_group = 0;                            // one group is the row
+    if (a.h_bf16) a.w_bf16 ? run_norm<true, true>(a, stream) : run_norm<true, false>(a, stream);
+    else a.w_bf16 ? run_norm<false, true>(a, stream) : run_norm<false, false>(a, stream);
     return hipGetLastError();
 }
 
 hipError_t launch_rmsnorm_backward(const NormGradArgs &a, hipStream_t stream)
 {
-    const int parts = norm_grad_parts(a.T, a.d);
+    const int parts = norm_grad_plan(a.T, a.d).groups;
     if (parts > 0) {
-        auto k = a.h_bf16 ? (a.w_bf16 ? norm_grad_kernel<true, true> : norm_grad_kernel<true, false>)
-                          : (a.w_bf16 ? norm_grad_kernel<false, true> : norm_grad_kernel<false, false>);
-        k<<<parts, NTH, 0, stream>>>(a);
+        if (a.h_bf16) a.w_bf16 ? run_grad<true, true>(a, parts, stream) : run_grad<true, false>(a, parts, stream);
+        else a.w_bf16 ? run_grad<false, true>(a, parts, stream) : run_grad<false, false>(a, parts, stream);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    norm_dw_kernel<<<(a.d + 63) / 64, 64, 0, stream>>>(a.part, a.dw, parts, a.d);
+    norm_dw_kernel<<<(a.d + 63) / 64, 256, 0, stream>>>(a.part, a.dw, parts, a.d);
     return hipGetLastError();
 }
 

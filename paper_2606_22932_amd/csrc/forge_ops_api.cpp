@@ -136,7 +136,7 @@ forge_status forge_rmsnorm(const void *x, const void *residual, const void *w, v
 
 int64_t forge_rmsnorm_backward_workspace(int64_t T, int64_t d)
 {
-    return check_rows(T, d) == FORGE_OK ? 4 * d * norm_grad_parts(T, d) : 0;
+    return check_rows(T, d) == FORGE_OK ? 4 * d * norm_grad_plan(T, d).groups : 0;
 }
 
 forge_status forge_rmsnorm_backward(const void *dy, const void *h, const void *w, const void *dres, void *dh, void *dx,

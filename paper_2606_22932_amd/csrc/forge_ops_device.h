@@ -6,43 +6,74 @@
 
 namespace forge_impl {
 
-// Eight elements from p[i ..] in registers.  bf16: 16 bytes; fp32: 32 bytes.
-template <bool BF16> __device__ __forceinline__ void load8(const void *p, size_t i, float (&f)[8])
-{
-    if constexpr (BF16) {
-        const u32x4_t u = *reinterpret_cast<const u32x4_t *>(static_cast<const uint16_t *>(p) + i);
+// N consecutive elements (4 or 8) from p[i ..] as they lie in memory, and as fp32 values.  bf16:
+// 2 N bytes in one access; fp32: 16 bytes an access.
+template <bool BF16, int N> struct Raw;
+template <int N> struct Raw<true, N> {
+    uint32_t u[N / 2];
+    __device__ __forceinline__ void load(const void *p, size_t i)
+    {
+        typedef uint32_t V __attribute__((ext_vector_type(N / 2)));
+        const V x = *reinterpret_cast<const V *>(static_cast<const uint16_t *>(p) + i);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            f[2 * k] = bf_lo(u[k]);
-            f[2 * k + 1] = bf_hi(u[k]);
-        }
-    } else {
-        const f32x4_t a = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(p) + i);
-        const f32x4_t b = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(p) + i + 4);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            f[k] = a[k];
-            f[4 + k] = b[k];
-        }
+        for (int k = 0; k < N / 2; ++k) u[k] = x[k];
     }
+    __device__ __forceinline__ float at(int k) const { return k & 1 ? bf_hi(u[k >> 1]) : bf_lo(u[k >> 1]); }
+    __device__ __forceinline__ void set(const float (&f)[N])
+    {
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k) u[k] = pack_bf16(f[2 * k], f[2 * k + 1]);
+    }
+    __device__ __forceinline__ void store(void *p, size_t i) const
+    {
+        typedef uint32_t V __attribute__((ext_vector_type(N / 2)));
+        V x;
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k) x[k] = u[k];
+        *reinterpret_cast<V *>(static_cast<uint16_t *>(p) + i) = x;
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k) u[k] = 0;
+    }
+};
+template <int N> struct Raw<false, N> {
+    f32x4_t v[N / 4];
+    __device__ __forceinline__ void load(const void *p, size_t i)
+    {
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) v[k] = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(p) + i + 4 * k);
+    }
+    __device__ __forceinline__ float at(int k) const { return v[k >> 2][k & 3]; }
+    __device__ __forceinline__ void set(const float (&f)[N])
+    {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k >> 2][k & 3] = f[k];
+    }
+    __device__ __forceinline__ void store(void *p, size_t i) const
+    {
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) *reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + i + 4 * k) = v[k];
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) v[k] = f32x4_t{0, 0, 0, 0};
+    }
+};
+template <bool BF16, int N> __device__ __forceinline__ void load_n(const void *p, size_t i, float (&f)[N])
+{
+    Raw<BF16, N> r;
+    r.load(p, i);
+#pragma unroll
+    for (int k = 0; k < N; ++k) f[k] = r.at(k);
 }
-template <bool BF16> __device__ __forceinline__ void store8(void *p, size_t i, const float (&f)[8])
+template <bool BF16, int N> __device__ __forceinline__ void store_n(void *p, size_t i, const float (&f)[N])
 {
-    if constexpr (BF16) {
-        u32x4_t u;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) u[k] = pack_bf16(f[2 * k], f[2 * k + 1]);
-        *reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(p) + i) = u;
-    } else {
-        f32x4_t a, b;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            a[k] = f[k];
-            b[k] = f[4 + k];
-        }
-        *reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + i) = a;
-        *reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + i + 4) = b;
-    }
+    Raw<BF16, N> r;
+    r.set(f);
+    r.store(p, i);
 }
 // x rounded to the stored type and back.
 template <bool BF16> __device__ __forceinline__ float as_stored(float x)
@@ -50,45 +81,50 @@ template <bool BF16> __device__ __forceinline__ float as_stored(float x)
     return BF16 ? (float)(__bf16)x : x;
 }
 
-// Sum over a workgroup of NT threads in a fixed order, to every thread.  `red` holds
-// NT / 64 floats and is free again after the caller's next barrier.
-template <int NT> __device__ __forceinline__ float group_sum(float x, float *red)
+// Lane exchanges without LDS round trips, for reductions over aligned groups of lanes: each step
+// gives a lane the value of one in the other half of a group twice as large, all lanes of a half
+// holding the same.  0xB1 and 0x4E are the quad permutations [1,0,3,2] and [2,3,0,1], 0x141
+// mirrors each half row of 8 lanes, 0x140 each row of 16.  Every lane must be active.
+template <int CTRL> __device__ __forceinline__ uint32_t lane_dpp(uint32_t x)
 {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = 0.0f;
-#pragma unroll
-    for (int k = 0; k < NT / 64; ++k) x += red[k];
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, true);
+}
+template <class F> __device__ __forceinline__ uint32_t lanes_join(uint32_t x, int lanes, F f)
+{
+    x = f(x, lane_dpp<0xB1>(x));
+    x = f(x, lane_dpp<0x4E>(x));
+    x = f(x, lane_dpp<0x141>(x));
+    if (lanes >= 16) x = f(x, lane_dpp<0x140>(x));
+    if (lanes >= 32) {
+        const auto h = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        x = f(h[0], h[1]);
+    }
+    if (lanes >= 64) {
+        const auto h = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        x = f(h[0], h[1]);
+    }
     return x;
+}
+// Sum or maximum over aligned groups of `lanes` (8, 16, 32 or 64) lanes, to all of them.
+__device__ __forceinline__ float lanes_sum(float x, int lanes)
+{
+    return __uint_as_float(lanes_join(__float_as_uint(x), lanes, [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x, int lanes)
+{
+    return lanes_join(x, lanes, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
 // Magnitudes are compared as bit patterns, which order like the values with Inf and then NaN
 // above them: a maximum over a block with a NaN is NaN.
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
-__device__ __forceinline__ uint32_t mag8(const float (&f)[8])
+template <int N> __device__ __forceinline__ uint32_t mag_n(const float (&f)[N])
 {
     uint32_t b = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) b = max(b, mag(f[k]));
-    return b;
-}
-// Maximum over aligned groups of `lanes` (a power of two) lanes, to all of them; every lane active.
-template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t b)
-{
-#pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) b = max(b, (uint32_t)__shfl_xor((int)b, o));
-    return b;
-}
-template <int NT> __device__ __forceinline__ uint32_t group_max(uint32_t b, uint32_t *red)
-{
-    b = lanes_max<64>(b);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = b;
-    __syncthreads();
-    b = 0;
-#pragma unroll
-    for (int k = 0; k < NT / 64; ++k) b = max(b, red[k]);
+    for (int k = 0; k < N; ++k) b = max(b, mag(f[k]));
     return b;
 }
 
@@ -105,25 +141,16 @@ __device__ __forceinline__ float e4m3_inverse(float scale)
     return scale > 0.0f ? __builtin_amdgcn_rcpf(scale) : 0.0f;
 }
 
-// Codes of eight values already divided by their scale, clamped to [lo, 448] first (the
-// hardware conversion gives NaN past 464), rounded to nearest even.
-__device__ __forceinline__ u32x2_t e4m3_encode8(const float (&x)[8], const float (&lo)[8])
+// Codes of values already divided by their scale, clamped to [lo, 448] first (the hardware
+// conversion gives NaN past 464), rounded to nearest even: four to a word.
+__device__ __forceinline__ uint32_t e4m3_encode4(float a, float b, float c, float d, float la = -448.0f,
+                                                 float lb = -448.0f, float lc = -448.0f, float ld = -448.0f)
 {
-    u32x2_t c;
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = __builtin_amdgcn_fmed3f(x[e], lo[e], 448.0f);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int h = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k], y[4 * k + 1], 0, false);
-        c[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2], y[4 * k + 3], h, true);
-    }
-    return c;
-}
-__device__ __forceinline__ u32x2_t e4m3_encode8(const float (&x)[8])
-{
-    const float lo[8] = {-448.0f, -448.0f, -448.0f, -448.0f, -448.0f, -448.0f, -448.0f, -448.0f};
-    return e4m3_encode8(x, lo);
+    a = __builtin_amdgcn_fmed3f(a, la, 448.0f);
+    b = __builtin_amdgcn_fmed3f(b, lb, 448.0f);
+    c = __builtin_amdgcn_fmed3f(c, lc, 448.0f);
+    d = __builtin_amdgcn_fmed3f(d, ld, 448.0f);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
 __device__ __forceinline__ void e4m3_decode8(const u32x2_t &c, float (&x)[8])
 {

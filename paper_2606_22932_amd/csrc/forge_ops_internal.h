@@ -30,7 +30,7 @@ struct NormGradArgs {
     void *dh;              // or null
     uint16_t *dx;          // or null
     float *dw;
-    float *part;           // [norm_grad_parts(T, d), d]
+    float *part;           // [norm_grad_plan(T, d).groups, d]
     int T, d;
     int h_bf16, w_bf16;
     float eps;
@@ -39,8 +39,32 @@ struct NormGradArgs {
 hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t stream);
 // T == 0 fills dw with zeros.
 hipError_t launch_rmsnorm_backward(const NormGradArgs &a, hipStream_t stream);
-// Rows of the partial sums of dw: how many workgroups share the T rows.
-inline int norm_grad_parts(int64_t T, int64_t) { return (int)(T < 512 ? T : 512); }
+
+// Columns of the widest row that the registers of a workgroup hold.
+constexpr int64_t NORM_WIDEST = 32768, GRAD_WIDEST = 16384;
+
+// A launch over T rows: workgroups, and threads of each.
+struct NormPlan {
+    int groups, threads;
+};
+// Rows that a wave holds at once: a lane has eight elements at least, a row eight lanes.
+inline int rows_per_wave(int64_t d) { return d <= 64 ? 8 : d <= 128 ? 4 : d <= 256 ? 2 : 1; }
+inline NormPlan norm_plan(int64_t T, int64_t d)
+{
+    const int64_t per = d > 4096 ? 1 : 4 * rows_per_wave(d), n = (T + per - 1) / per;
+    return {(int)(n < 2048 ? n : 2048), d > 16384 ? 1024 : 256};
+}
+// The gradient's workgroups each leave a row of partial sums of dw: at most two for each CU, so
+// that these stay small beside the rows, and as many rows at once in each as there are for all.
+inline NormPlan norm_grad_plan(int64_t T, int64_t d)
+{
+    if (d > GRAD_WIDEST) return {(int)(T < 512 ? T : 512), 256};
+    const int64_t waves = d <= 1024 ? 1 : d <= 2048 ? 2 : d <= 4096 ? 4 : d <= 8192 ? 8 : 16;   // of a row
+    int64_t rows = 1;
+    while (waves * rows < 8 && T > 256 * rows * rows_per_wave(d)) rows *= 2;
+    const int64_t per = rows * rows_per_wave(d), n = (T + per - 1) / per;
+    return {(int)(n < 512 ? n : 512), (int)(64 * waves * rows)};
+}
 
 // ------------------------------------------------------------------------ many tensors
 
