@@ -64,6 +64,31 @@ __device__ __forceinline__ void store_codes(void *p, size_t i, int n, const u32x
     }
 }
 
+// sqrt(x) rounded to nearest: the product with the reciprocal root, corrected by the exact
+// remainder once.  Against the fp64 root over every fp32 mantissa, with the hardware's result and
+// its two neighbours: another value in 5 of 50331648 cases, one step off.  Small x are taken
+// times 2^64, so that no remainder underflows.
+__device__ __forceinline__ float rounded_root(float x)
+{
+    const bool small = x < 0x1p-96f;
+    const float z = small ? x * 0x1p64f : x;
+    const float h = __builtin_amdgcn_rsqf(fmaxf(z, 0x1p-126f));
+    const float y = z * h, root = __builtin_fmaf(__builtin_fmaf(-y, y, z), 0.5f * h, y);
+    return z < __builtin_inff() ? (small ? root * 0x1p-32f : root) : z;      // Inf and NaN as they are
+}
+// x / s rounded to nearest from i = RN(1 / s): again one correction by the exact remainder (no
+// difference from IEEE division in 2.4e8 cases, i off by a step or not before its refinement).
+__device__ __forceinline__ float refined_inverse(float s)
+{
+    const float i = e4m3_inverse(s);
+    return __builtin_fmaf(__builtin_fmaf(-s, i, 1.0f), i, i);
+}
+__device__ __forceinline__ float rounded_quotient(float x, float s, float i)
+{
+    const float q = x * i;
+    return __builtin_fmaf(__builtin_fmaf(-q, s, x), i, q);
+}
+
 // One AdamW element (Algorithm 1).  fp32 and bf16 state: the arithmetic of forge_adamw's kernels
 // to the bit.  fp8 state: every operation up to the codes is one IEEE fp32 operation, none of
 // them fused, the root and the quotient by the scale correctly rounded.  Next to the border of
@@ -76,7 +101,7 @@ __device__ __forceinline__ void adamw1(float g, float &w, float &m, float &v, fl
     if constexpr (EXACT) {
         m = h.b1 * m + h.c1 * g;
         v = h.b2 * v + h.c2 * (g * g);
-        root = sqrtf(v);
+        root = rounded_root(v);
     } else {
         m = __builtin_fmaf(h.b1, m, h.c1 * g);
         v = __builtin_fmaf(h.b2, v, (h.c2 * g) * g);
@@ -122,6 +147,7 @@ __device__ __forceinline__ void adamw_chunk(const MtTensor &t, size_t i, int n, 
             if (k >= n) m[k] = root[k] = 0.0f;
         const float ms = e4m3_scale(lanes_max(mag_n(m), 8));
         const float vs = e4m3_scale(lanes_max(mag_n(root), 8));
+        const float mi = refined_inverse(ms), vi = refined_inverse(vs);
         float lo[8];
         if (n > 0 && i % MT_BLOCK == 0) {
             t.ms[i / MT_BLOCK] = ms;
@@ -129,9 +155,9 @@ __device__ __forceinline__ void adamw_chunk(const MtTensor &t, size_t i, int n, 
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            m[k] = ms > 0.0f ? m[k] / ms : 0.0f;
+            m[k] = rounded_quotient(m[k], ms, mi);
             lo[k] = root[k] > 0.0f ? 0x1p-9f : 0.0f;      // a sqrt(v) > 0 is not stored as zero
-            root[k] = vs > 0.0f ? root[k] / vs : 0.0f;
+            root[k] = rounded_quotient(root[k], vs, vi);
         }
         store_codes(t.m, i, n, u32x2_t{e4m3_encode4(m[0], m[1], m[2], m[3]), e4m3_encode4(m[4], m[5], m[6], m[7])});
         store_codes(t.v, i, n, u32x2_t{e4m3_encode4(root[0], root[1], root[2], root[3], lo[0], lo[1], lo[2], lo[3]),

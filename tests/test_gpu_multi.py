@@ -157,11 +157,12 @@ def test_bits_of_forge_adamw(state, g):
             assert torch.equal(new[k].view(torch.uint8), t.one[k].cpu().view(-1).view(torch.uint8)), k
 
 
-@pytest.mark.parametrize("g", ["bf16", "f32"])
-def test_fp8_state_to_the_bit(g):
+@pytest.mark.parametrize("g,cold,size", [("bf16", False, 0.1), ("f32", False, 0.1), ("f32", True, 1e-17), ("f32", True, 1e-13)])
+def test_fp8_state_to_the_bit(g, cold, size):
     """Codes and scales are those of plain fp32 arithmetic, over several steps that each read the
-    codes of the one before: a last bit lost anywhere would change some of half a million codes."""
-    t = Tensor(500033, "f32", g, "fp8", seed=21)
+    codes of the one before: a last bit lost anywhere would change some of half a million codes.
+    From cold state with tiny gradients v lies about the smallest normal number."""
+    t = Tensor(500033, "f32", g, "fp8", seed=21, cold=cold)
     lst = forge.TensorList([t.entry()])
     coef = torch.tensor([0.37])
     f = torch.float32
@@ -179,7 +180,8 @@ def test_fp8_state_to_the_bit(g):
 
     q = {k: t.host[k] for k in ("m", "v", "ms", "vs")}
     for step in range(2, 6):
-        grad = rand(t.n, 10.0 ** -step, 70 + step).to(DT[g])
+        grad = rand(t.n, size * 10.0 ** -step, 70 + step).to(DT[g])
+        grad[64 * step:64 * step + 64] = 0.0 if step < 4 else 1e-20        # and blocks of tiny numbers
         t.dev["G"].copy_(grad)
         t.host["G"] = grad
         forge.forge_adamw_multi(lst, step=step, grad_scale=coef.cuda(), **HP)
