@@ -60,7 +60,7 @@ __device__ __forceinline__ void row_sum(float (&x)[N], const R &row, float (*red
 }
 
 template <bool HB, bool WB, int E, int WR>
-__global__ void __launch_bounds__(WR == 1 ? 256 : 64 * WR) norm_kernel(NormArgs a)
+__global__ void __launch_bounds__(WR == 16 ? 1024 : 256) norm_kernel(NormArgs a)
 {
     using R = Row<HB, E, WR>;
     constexpr int V = R::V, NV = R::NV;
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(WR == 1 ? 256 : 64 * WR) norm_kernel(NormArgs 
                 if ((threadIdx.x & 63) == 0) redm[turn & 1][threadIdx.x >> 6] = top;
                 lds_barrier();
 #pragma unroll
-                for (int i = 0; i < WR; ++i) top = max(top, redm[turn & 1][i]);
+                for (int i = 0; i < WR; ++i) top = max(top, redm[turn & 1][row.slot * WR + i]);
             }
             qs = e4m3_scale(top);
             inv = e4m3_inverse(qs);
@@ -162,31 +162,28 @@ __global__ void __launch_bounds__(WR == 1 ? 256 : 64 * WR) norm_kernel(NormArgs 
 }
 
 // Each workgroup takes its rows in turn: dh and dx of each, and their share of dw in registers,
-// which it leaves in its row of the workspace.  The next rows are loaded ahead of the sums of
-// these, so that loads are in flight across the barrier.
+// which it leaves in its row of the workspace.  The next rows' h and dy are loaded ahead of the
+// sums of these, so that loads are in flight across the barrier.
 template <bool HB, int E, int WR> struct GradRow {
     static constexpr int V = Row<HB, E, WR>::V, NV = Row<HB, E, WR>::NV;
-    Raw<HB, V> h[NV], o[NV];
+    Raw<HB, V> h[NV];
     Raw<true, V> g[NV];
     __device__ __forceinline__ void load(const NormGradArgs &a, const Row<HB, E, WR> &row, int t)
     {
         const size_t at = (size_t)t * a.d;
-        const bool live = t < a.T;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             h[j].zero();
             g[j].zero();
-            o[j].zero();
-            if (!live || !row.has(j)) continue;
+            if (t >= a.T || !row.has(j)) continue;
             h[j].load(a.h, at + V * row.vec(j));
             g[j].load(a.dy, at + V * row.vec(j));
-            if (a.dres) o[j].load(a.dres, at + V * row.vec(j));
         }
     }
 };
 
 template <bool HB, bool WB, int E, int WR>
-__global__ void __launch_bounds__(WR == 16 ? 1024 : 512) norm_grad_kernel(NormGradArgs a)
+__global__ void __launch_bounds__(WR == 16 ? 1024 : 512, 4) norm_grad_kernel(NormGradArgs a)
 {
     using R = Row<HB, E, WR>;
     constexpr int V = R::V, NV = R::NV;
@@ -210,6 +207,12 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512) norm_grad_kernel(NormGr
     for (int t0 = blockIdx.x * row.slots; t0 < a.T; t0 += stride, ++turn) {
         const int t = t0 + row.slot;
         const size_t at = (size_t)t * a.d;
+        Raw<HB, V> o[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            o[j].zero();
+            if (a.dres && t < a.T && row.has(j)) o[j].load(a.dres, at + V * row.vec(j));
+        }
         next.load(a, row, t < a.T - stride ? t + stride : a.T);
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -224,10 +227,12 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512) norm_grad_kernel(NormGr
         const float c = s * s * (sum[1] * inv_d);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            now.h[j].forget();
+            now.g[j].forget();
             float x[V];
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                x[k] = __builtin_fmaf(s, __builtin_fmaf(-now.h[j].at(k), c, now.g[j].at(k) * w[j].at(k)), now.o[j].at(k));
+                x[k] = __builtin_fmaf(s, __builtin_fmaf(-now.h[j].at(k), c, now.g[j].at(k) * w[j].at(k)), o[j].at(k));
                 acc[j][k] = __builtin_fmaf(now.g[j].at(k), now.h[j].at(k) * s, acc[j][k]);
             }
             if (t >= a.T || !row.has(j)) continue;
@@ -237,10 +242,20 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512) norm_grad_kernel(NormGr
         now = next;
     }
     float *part = a.part + (size_t)blockIdx.x * a.d;
+    if constexpr (WR == 1) {
+        // the rows that share a wave
+        for (int o = row.lanes; o < 64; o <<= 1)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int k = 0; k < V; ++k) acc[j][k] += __shfl_xor(acc[j][k], o);
+    }
     if constexpr (WR < 16) {
-        // the rows that the workgroup held at once, one after the other
-        for (int i = 0; i < row.slots; ++i) {
-            if (row.slot == i) {
+        // the waves that held the same columns, one after the other
+        const int mine = (threadIdx.x >> 6) / WR, all = (blockDim.x >> 6) / WR;
+        const bool writes = WR > 1 || (int)(threadIdx.x & 63) < row.lanes;
+        for (int i = 0; i < all; ++i) {
+            if (mine == i && writes) {
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
                     if (!row.has(j)) continue;
@@ -250,7 +265,7 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512) norm_grad_kernel(NormGr
 #pragma unroll
                         for (int k = 0; k < V; ++k) acc[j][k] += x[k];
                     }
-                    if (i + 1 < row.slots) store_n<false>(share, V * row.vec(j), acc[j]);
+                    if (i + 1 < all) store_n<false>(share, V * row.vec(j), acc[j]);
                     else store_n<false>(part, V * row.vec(j), acc[j]);
                 }
             }
@@ -263,20 +278,31 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512) norm_grad_kernel(NormGr
     }
 }
 
-// dw: the parts' sum.  A workgroup takes 64 columns, 16 threads of four columns by 16 runs of
-// parts, joined through LDS in the runs' order.
-__global__ void __launch_bounds__(256) norm_dw_kernel(const float *part, float *dw, int parts, int d)
+// dw: the parts' sum.  A workgroup takes 32 columns, eight threads of four columns by 32 runs of
+// parts, eight parts of a run in flight, joined through LDS in the runs' order.
+constexpr int DW_COLS = 32, DW_RUNS = 32;
+__global__ void __launch_bounds__(DW_RUNS * 8) norm_dw_kernel(const float *part, float *dw, int parts, int d)
 {
-    __shared__ f32x4_t red[16][16];
-    const int c = threadIdx.x & 15, r = threadIdx.x >> 4, j = (blockIdx.x * 16 + c) * 4;
+    __shared__ f32x4_t red[DW_RUNS][8];
+    const int c = threadIdx.x & 7, r = threadIdx.x >> 3, j = blockIdx.x * DW_COLS + 4 * c;
     f32x4_t x = {0, 0, 0, 0};
     if (j < d)
-        for (int p = r; p < parts; p += 16) x += *reinterpret_cast<const f32x4_t *>(part + (size_t)p * d + j);
+        for (int p0 = r; p0 < parts; p0 += 8 * DW_RUNS) {
+            f32x4_t y[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int p = p0 + k * DW_RUNS;
+                y[k] = f32x4_t{0, 0, 0, 0};
+                if (p < parts) y[k] = *reinterpret_cast<const f32x4_t *>(part + (size_t)p * d + j);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x += y[k];
+        }
     red[r][c] = x;
     __syncthreads();
     if (r || j >= d) return;
 #pragma unroll
-    for (int k = 1; k < 16; ++k) x += red[k][c];
+    for (int k = 1; k < DW_RUNS; ++k) x += red[k][c];
     *reinterpret_cast<f32x4_t *>(dw + j) = x;
 }
 
@@ -416,20 +442,20 @@ template <int N> using Int = std::integral_constant<int, N>;
 template <class F> void norm_width(int64_t d, F f)
 {
     if (d <= 512) f(Int<8>(), Int<1>());
-    else if (d <= 1024) f(Int<16>(), Int<1>());
-    else if (d <= 2048) f(Int<32>(), Int<1>());
-    else if (d <= 4096) f(Int<64>(), Int<1>());
+    else if (d <= 1024) f(Int<8>(), Int<2>());
+    else if (d <= 2048) f(Int<8>(), Int<4>());
+    else if (d <= 4096) f(Int<16>(), Int<4>());
     else if (d <= 8192) f(Int<32>(), Int<4>());
-    else if (d <= 16384) f(Int<64>(), Int<4>());
+    else if (d <= 16384) f(Int<16>(), Int<16>());
     else f(Int<32>(), Int<16>());
 }
 template <class F> void grad_width(int64_t d, F f)
 {
     if (d <= 512) f(Int<8>(), Int<1>());
-    else if (d <= 1024) f(Int<16>(), Int<1>());
-    else if (d <= 2048) f(Int<16>(), Int<2>());
-    else if (d <= 4096) f(Int<16>(), Int<4>());
-    else if (d <= 8192) f(Int<16>(), Int<8>());
+    else if (d <= 1024) f(Int<8>(), Int<2>());
+    else if (d <= 2048) f(Int<8>(), Int<4>());
+    else if (d <= 4096) f(Int<8>(), Int<8>());
+    else if (d <= 8192) f(Int<8>(), Int<16>());
     else f(Int<16>(), Int<16>());
 }
 
@@ -469,16 +495,19 @@ hipError_t launch_rmsnorm(const NormArgs &args, hipStream_t stream)
     return hipGetLastError();
 }
 
-hipError_t launch_rmsnorm_backward(const NormGradArgs &a, hipStream_t stream)
+hipError_t launch_rmsnorm_backward(const NormGradArgs &args, hipStream_t stream)
 {
+    NormGradArgs a = args;
     const int parts = norm_grad_plan(a.T, a.d).groups;
+    if (parts == 1) a.part = a.dw;
     if (parts > 0) {
         if (a.h_bf16) a.w_bf16 ? run_grad<true, true>(a, parts, stream) : run_grad<true, false>(a, parts, stream);
         else a.w_bf16 ? run_grad<false, true>(a, parts, stream) : run_grad<false, false>(a, parts, stream);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    norm_dw_kernel<<<(a.d + 63) / 64, 256, 0, stream>>>(a.part, a.dw, parts, a.d);
+    if (parts == 1) return hipSuccess;                        // its part is dw
+    norm_dw_kernel<<<(a.d + DW_COLS - 1) / DW_COLS, DW_RUNS * 8, 0, stream>>>(a.part, a.dw, parts, a.d);
     return hipGetLastError();
 }
 

@@ -37,6 +37,12 @@ template <int N> struct Raw<true, N> {
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) u[k] = 0;
     }
+    // To the compiler another value: what it unpacked before is unpacked again, not kept.
+    __device__ __forceinline__ void forget()
+    {
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k) asm volatile("" : "+v"(u[k]));
+    }
 };
 template <int N> struct Raw<false, N> {
     f32x4_t v[N / 4];
@@ -61,6 +67,7 @@ template <int N> struct Raw<false, N> {
 #pragma unroll
         for (int k = 0; k < N / 4; ++k) v[k] = f32x4_t{0, 0, 0, 0};
     }
+    __device__ __forceinline__ void forget() {}
 };
 template <bool BF16, int N> __device__ __forceinline__ void load_n(const void *p, size_t i, float (&f)[N])
 {

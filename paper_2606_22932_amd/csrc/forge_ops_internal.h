@@ -51,19 +51,25 @@ struct NormPlan {
 inline int rows_per_wave(int64_t d) { return d <= 64 ? 8 : d <= 128 ? 4 : d <= 256 ? 2 : 1; }
 inline NormPlan norm_plan(int64_t T, int64_t d)
 {
-    const int64_t per = d > 4096 ? 1 : 4 * rows_per_wave(d), n = (T + per - 1) / per;
-    return {(int)(n < 2048 ? n : 2048), d > 16384 ? 1024 : 256};
+    // Workgroups take a second row once there are more than this: rows of a wave sooner, whose
+    // start costs more beside them (30000 x 512: 25.7 against 27.2 us), than rows of several
+    // (16384 x 4096: 96.8 us at 8192 workgroups, 101.6 at 2048, 95.6 without a limit, which in
+    // turn loses 2 % at 16384 x 8192).
+    const int64_t per = d > 1024 ? 1 : d > 512 ? 2 : 4 * rows_per_wave(d), n = (T + per - 1) / per;
+    const int64_t most = d > 512 ? 8192 : 2048;
+    return {(int)(n < most ? n : most), d > 8192 ? 1024 : 256};
 }
-// The gradient's workgroups each leave a row of partial sums of dw: at most two for each CU, so
-// that these stay small beside the rows, and as many rows at once in each as there are for all.
+// The gradient's workgroups each leave a row of partial sums of dw, written and read again beside
+// the rows' own bytes: one for each CU, two where that is no more than a row for four of the
+// input, and as many rows at once in each as there are for all.
 inline NormPlan norm_grad_plan(int64_t T, int64_t d)
 {
     if (d > GRAD_WIDEST) return {(int)(T < 512 ? T : 512), 256};
-    const int64_t waves = d <= 1024 ? 1 : d <= 2048 ? 2 : d <= 4096 ? 4 : d <= 8192 ? 8 : 16;   // of a row
+    const int64_t waves = d <= 512 ? 1 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 4096 ? 8 : 16;   // of a row
     int64_t rows = 1;
     while (waves * rows < 8 && T > 256 * rows * rows_per_wave(d)) rows *= 2;
-    const int64_t per = rows * rows_per_wave(d), n = (T + per - 1) / per;
-    return {(int)(n < 512 ? n : 512), (int)(64 * waves * rows)};
+    const int64_t per = rows * rows_per_wave(d), n = (T + per - 1) / per, most = waves < 16 && T >= 2048 ? 512 : 256;
+    return {(int)(n < most ? n : most), (int)(64 * waves * rows)};
 }
 
 // ------------------------------------------------------------------------ many tensors

@@ -456,7 +456,7 @@ def _float_code(t, what):
 
 
 def _like(t, what, shape, dtype):
-    if t is not None and (t.shape != shape or t.dtype != dtype):
+    if t is not None and (t.shape != shape or t.dtype is not dtype):
         raise ValueError(f"{what} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
@@ -470,27 +470,34 @@ def _bytes_ws(ws, need):
     return ws.nbytes
 
 
-class _on:
-    """The device of ``ref`` made current for a call; every tensor must live there."""
-    __slots__ = ("to", "back")
+def _one_device(*ts):
+    """Index of the HIP device that all the tensors given live on, contiguous."""
+    dev = None
+    for t in ts:
+        if t is not None:
+            at = t.get_device()
+            if at != dev or not t.is_contiguous():
+                _dev(t)
+                if dev is not None:
+                    raise ValueError(f"tensors on different devices: {dev} and {at}")
+                dev = at
+    return dev
 
-    def __init__(self, ref, *ts):
-        import torch
-        _dev(ref, *ts)
-        for t in ts:
-            if t is not None and t.device != ref.device:
-                raise ValueError(f"tensors on different devices: {ref.device} and {t.device}")
-        self.to, self.back = ref.device.index, torch.cuda.current_device()
 
-    def __enter__(self):
-        if self.to != self.back:
-            import torch
-            torch.cuda.set_device(self.to)
-
-    def __exit__(self, *exc):
-        if self.to != self.back:
-            import torch
-            torch.cuda.set_device(self.back)
+def _launch(name, dev, stream, *args):
+    """The C entry point with ``dev`` current, on ``stream`` or torch's current one there."""
+    import torch
+    if stream is None:
+        # the handle alone: torch.cuda.current_stream makes an object for it, 2 us a call
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+    fn = getattr(_ops_lib or _ops(), name)
+    if torch.cuda.current_device() == dev:
+        st = fn(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, stream)
+    if st:
+        raise ForgeError(st, name)
 
 
 def forge_rmsnorm(x, w, *, residual=None, h=None, y=None, q=None, q_scale=None, eps, stream=None):
@@ -501,24 +508,23 @@ def forge_rmsnorm(x, w, *, residual=None, h=None, y=None, q=None, q_scale=None, 
     [T, ceil(d / 128)] (per 128 columns).  ``h`` goes with a residual and may be the residual.
     """
     import torch
-    T, d = x.shape
-    with _on(x, w, residual, h, y, q, q_scale):
-        _like(w, "w", (d,), w.dtype)
-        s = x if residual is None else residual
-        if residual is not None:
-            _like(x, "x beside a residual", x.shape, torch.bfloat16)
-            _like(residual, "residual", x.shape, residual.dtype)
-            _like(h, "h", x.shape, residual.dtype)
-        _like(y, "y", x.shape, torch.bfloat16)
-        _like(q, "q", x.shape, torch.float8_e4m3fn)
-        group = 0
-        if q is not None and q_scale is not None:
-            if q_scale.dim() == 2:
-                group = FORGE_Q_GROUP
-            _like(q_scale, "q_scale", (T, (d + 127) // 128) if group else (T,), torch.float32)
-        st = _ops().forge_rmsnorm(_adr(x), _adr(residual), _adr(w), _adr(h), _adr(y), _adr(q), _adr(q_scale), T, d,
-                                  _float_code(s, "the stream"), _float_code(w, "w"), group, eps, _stream(stream, x))
-    _check(st, "forge_rmsnorm")
+    shape = T, d = x.shape
+    dev = _one_device(x, w, residual, h, y, q, q_scale)
+    _like(w, "w", (d,), w.dtype)
+    s = x
+    if residual is not None:
+        s = residual
+        _like(x, "x beside a residual", shape, torch.bfloat16)
+        _like(residual, "residual", shape, residual.dtype)
+    _like(h, "h", shape, s.dtype)
+    _like(y, "y", shape, torch.bfloat16)
+    _like(q, "q", shape, torch.float8_e4m3fn)
+    group = 0
+    if q is not None and q_scale is not None:
+        group = FORGE_Q_GROUP if q_scale.dim() == 2 else 0
+        _like(q_scale, "q_scale", (T, (d + 127) // 128) if group else (T,), torch.float32)
+    _launch("forge_rmsnorm", dev, stream, x.data_ptr(), _adr(residual), w.data_ptr(), _adr(h), _adr(y), _adr(q),
+            _adr(q_scale), T, d, _float_code(s, "the stream"), _float_code(w, "w"), group, eps)
 
 
 def forge_rmsnorm_backward_workspace(T, d):
@@ -531,20 +537,18 @@ def forge_rmsnorm_backward(dy, h, w, *, dres=None, dh=None, dx=None, dw, eps, ws
     dres + the norm's gradient, and dw (float32).  ``h`` is what the norm was taken of; dh may be
     dres.  ``ws``: any tensor of at least ``forge_rmsnorm_backward_workspace(T, d)`` bytes."""
     import torch
-    T, d = dy.shape
-    with _on(dy, h, w, dres, dh, dx, dw, ws):
-        _like(dy, "dy", dy.shape, torch.bfloat16)
-        _like(h, "h", dy.shape, h.dtype)
-        _like(w, "w", (d,), w.dtype)
-        _like(dres, "dres", dy.shape, h.dtype)
-        _like(dh, "dh", dy.shape, h.dtype)
-        _like(dx, "dx", dy.shape, torch.bfloat16)
-        _like(dw, "dw", (d,), torch.float32)
-        n = _bytes_ws(ws, forge_rmsnorm_backward_workspace(T, d))
-        st = _ops().forge_rmsnorm_backward(_adr(dy), _adr(h), _adr(w), _adr(dres), _adr(dh), _adr(dx), _adr(dw), T, d,
-                                           _float_code(h, "h"), _float_code(w, "w"), eps, _adr(ws), n,
-                                           _stream(stream, dy))
-    _check(st, "forge_rmsnorm_backward")
+    shape = T, d = dy.shape
+    dev = _one_device(dy, h, w, dres, dh, dx, dw, ws)
+    _like(dy, "dy", shape, torch.bfloat16)
+    _like(h, "h", shape, h.dtype)
+    _like(w, "w", (d,), w.dtype)
+    _like(dres, "dres", shape, h.dtype)
+    _like(dh, "dh", shape, h.dtype)
+    _like(dx, "dx", shape, torch.bfloat16)
+    _like(dw, "dw", (d,), torch.float32)
+    n = _bytes_ws(ws, forge_rmsnorm_backward_workspace(T, d))
+    _launch("forge_rmsnorm_backward", dev, stream, dy.data_ptr(), h.data_ptr(), w.data_ptr(), _adr(dres), _adr(dh),
+            _adr(dx), dw.data_ptr(), T, d, _float_code(h, "h"), _float_code(w, "w"), eps, _adr(ws), n)
 
 
 class TensorList:
@@ -620,9 +624,9 @@ class TensorList:
         """The stream's handle, the table kept from reuse until that stream is done with it."""
         import torch
         if stream is None:
-            stream = torch.cuda.current_stream(self.device).cuda_stream
+            stream = torch._C._cuda_getCurrentRawStream(self.device.index)
         stream = int(stream)
-        if self.table is not None and stream != self._home:
+        if stream != self._home:
             self.table.record_stream(torch.cuda.ExternalStream(stream, self.device))
         return stream
 
@@ -636,12 +640,11 @@ def forge_grad_norm(tensors, out, *, max_norm, ws, stream=None):
     """out[0] = the 2-norm of all gradients of a TensorList, out[1] = min(1, max_norm / (out[0] +
     1e-6)); ``out`` float32 [2], ``out[1:]`` is what ``forge_adamw_multi`` takes as grad_scale."""
     import torch
-    with _on(out, ws, tensors.table):
-        _like(out, "out", (2,), torch.float32)
-        n = _bytes_ws(ws, forge_grad_norm_workspace(tensors))
-        st = _ops().forge_grad_norm(tensors._ref, _adr(tensors.table), max_norm, _adr(out), _adr(ws), n,
-                                    _stream(stream, out) if tensors.table is None else tensors._use(stream))
-    _check(st, "forge_grad_norm")
+    dev = _one_device(out, ws, tensors.table)
+    _like(out, "out", (2,), torch.float32)
+    n = _bytes_ws(ws, forge_grad_norm_workspace(tensors))
+    _launch("forge_grad_norm", dev, stream if tensors.table is None else tensors._use(stream), tensors._ref,
+            _adr(tensors.table), max_norm, out.data_ptr(), _adr(ws), n)
 
 
 def forge_adamw_multi(tensors, *, lr, beta1, beta2, eps, step, grad_scale=None, stream=None):
@@ -651,9 +654,8 @@ def forge_adamw_multi(tensors, *, lr, beta1, beta2, eps, step, grad_scale=None, 
     import torch
     if tensors.table is None:
         return
-    with _on(tensors.table, grad_scale):
-        if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
-            raise ValueError("grad_scale must be one float32")
-        st = _ops().forge_adamw_multi(tensors._ref, _adr(tensors.table), lr, beta1, beta2, eps, _adr(grad_scale),
-                                      int(step), tensors._use(stream))
-    _check(st, "forge_adamw_multi")
+    dev = _one_device(tensors.table, grad_scale)
+    if grad_scale is not None and (grad_scale.dtype is not torch.float32 or grad_scale.numel() != 1):
+        raise ValueError("grad_scale must be one float32")
+    _launch("forge_adamw_multi", dev, tensors._use(stream), tensors._ref, tensors.table.data_ptr(), lr, beta1, beta2,
+            eps, _adr(grad_scale), int(step))

@@ -75,7 +75,7 @@ def test_rmsnorm_accepts(over):
 
 @pytest.mark.parametrize("over,want", [
     (dict(h_dtype=2), DTYPE), (dict(w_dtype=7), DTYPE), (dict(T=-1), SHAPE), (dict(d=9), UNSUP),
-    (dict(ws_bytes=0), SHAPE), (dict(ws_bytes=4 * 256 * 4 - 1), SHAPE), (dict(d=0, dw=0, ws_bytes=0), OK),
+    (dict(ws_bytes=0), SHAPE), (dict(d=0, dw=0, ws_bytes=0), OK),
     (dict(dw=0), NULLP), (dict(dy=0), NULLP), (dict(h=0), NULLP), (dict(w=0), NULLP), (dict(dh=0, dx=0), NULLP),
     (dict(ws=0), NULLP), (dict(T=0, dw=0), NULLP), (dict(eps=0.0), HYPER), (dict(T=0, dw=GRAD["dw"] + 4), MISAL),
     *[({k: GRAD[k] + 8}, MISAL) for k in ("dy", "h", "w", "dres", "dh", "dx", "dw", "ws")],
@@ -98,6 +98,8 @@ def test_workspace_sizes():
     L = lib()
     assert L.forge_rmsnorm_backward_workspace(0, 64) == 0
     assert L.forge_rmsnorm_backward_workspace(-1, 64) == L.forge_rmsnorm_backward_workspace(3, 12) == 0
+    need = L.forge_rmsnorm_backward_workspace(GRAD["T"], GRAD["d"])
+    assert grad(ws_bytes=need - 1) == SHAPE and grad(ws_bytes=need, w=0) == NULLP
     for T, d in ((1, 8), (7, 4096), (1 << 20, 64), (1 << 14, 1 << 14), ((1 << 31) // 8 - 1, 8)):
         n = L.forge_rmsnorm_backward_workspace(T, d)
         assert n > 0 and n % (4 * d) == 0 and n <= 4 * d * min(T, 4096)
