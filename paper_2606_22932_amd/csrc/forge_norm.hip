@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 256) norm_kernel(NormArgs a)
 #pragma unroll
                     for (int k = 0; k < V; ++k) f[j][k] = r[j].at(k) + x[j].at(k);
                     r[j].set(f[j]);
-                    if (live && row.has(j)) r[j].store(a.h, at + V * row.vec(j));
+                    if (live && row.has(j)) r[j].template store<true>(a.h, at + V * row.vec(j));
                 }
             } else {
 #pragma unroll
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 256) norm_kernel(NormArgs a)
 // Each workgroup takes its rows in turn: dh and dx of each, and their share of dw in registers,
 // which it leaves in its row of the workspace.  The next rows' h and dy are loaded ahead of the
 // sums of these, so that loads are in flight across the barrier.
-template <bool HB, int E, int WR> struct GradRow {
+template <bool HB, bool NT, int E, int WR> struct GradRow {
     static constexpr int V = Row<HB, E, WR>::V, NV = Row<HB, E, WR>::NV;
     Raw<HB, V> h[NV];
     Raw<true, V> g[NV];
@@ -176,13 +176,13 @@ template <bool HB, int E, int WR> struct GradRow {
             h[j].zero();
             g[j].zero();
             if (t >= a.T || !row.has(j)) continue;
-            h[j].load(a.h, at + V * row.vec(j));
-            g[j].load(a.dy, at + V * row.vec(j));
+            h[j].template load<NT>(a.h, at + V * row.vec(j));
+            g[j].template load<NT>(a.dy, at + V * row.vec(j));
         }
     }
 };
 
-template <bool HB, bool WB, int E, int WR>
+template <bool HB, bool WB, bool NT, int E, int WR>
 __global__ void __launch_bounds__(WR == 16 ? 1024 : 512, 4) norm_grad_kernel(NormGradArgs a)
 {
     using R = Row<HB, E, WR>;
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512, 4) norm_grad_kernel(Nor
 #pragma unroll
         for (int k = 0; k < V; ++k) acc[j][k] = 0.0f;
     }
-    GradRow<HB, E, WR> now, next;
+    GradRow<HB, NT, E, WR> now, next;
     now.load(a, row, blockIdx.x * row.slots + row.slot);
     int turn = 0;
     for (int t0 = blockIdx.x * row.slots; t0 < a.T; t0 += stride, ++turn) {
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512, 4) norm_grad_kernel(Nor
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             o[j].zero();
-            if (a.dres && t < a.T && row.has(j)) o[j].load(a.dres, at + V * row.vec(j));
+            if (a.dres && t < a.T && row.has(j)) o[j].template load<NT>(a.dres, at + V * row.vec(j));
         }
         next.load(a, row, t < a.T - stride ? t + stride : a.T);
         float sum[2] = {0.0f, 0.0f};
@@ -480,7 +480,9 @@ template <bool HB, bool WB> void run_grad(const NormGradArgs &a, int parts, hipS
     }
     grad_width(a.d, [&](auto e, auto wr) {
         constexpr int E = decltype(e)::value, WR = decltype(wr)::value;
-        norm_grad_kernel<HB, WB, E, WR><<<parts, norm_grad_plan(a.T, a.d).threads, 0, stream>>>(a);
+        const int threads = norm_grad_plan(a.T, a.d).threads;
+        if ((int64_t)a.T * a.d * (HB ? 6 : 10) > GRAD_CACHED) norm_grad_kernel<HB, WB, true, E, WR><<<parts, threads, 0, stream>>>(a);
+        else norm_grad_kernel<HB, WB, false, E, WR><<<parts, threads, 0, stream>>>(a);
     });
 }
 

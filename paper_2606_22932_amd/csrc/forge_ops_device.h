@@ -6,15 +6,26 @@
 
 namespace forge_impl {
 
+template <bool NT, class V> __device__ __forceinline__ V load_v(const V *p)
+{
+    if constexpr (NT) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool NT, class V> __device__ __forceinline__ void store_v(V *p, V x)
+{
+    if constexpr (NT) __builtin_nontemporal_store(x, p);
+    else *p = x;
+}
+
 // N consecutive elements (4 or 8) from p[i ..] as they lie in memory, and as fp32 values.  bf16:
-// 2 N bytes in one access; fp32: 16 bytes an access.
+// 2 N bytes in one access; fp32: 16 bytes an access.  NT: non-temporal.
 template <bool BF16, int N> struct Raw;
 template <int N> struct Raw<true, N> {
     uint32_t u[N / 2];
-    __device__ __forceinline__ void load(const void *p, size_t i)
+    template <bool NT = false> __device__ __forceinline__ void load(const void *p, size_t i)
     {
         typedef uint32_t V __attribute__((ext_vector_type(N / 2)));
-        const V x = *reinterpret_cast<const V *>(static_cast<const uint16_t *>(p) + i);
+        const V x = load_v<NT>(reinterpret_cast<const V *>(static_cast<const uint16_t *>(p) + i));
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) u[k] = x[k];
     }
@@ -24,13 +35,13 @@ template <int N> struct Raw<true, N> {
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) u[k] = pack_bf16(f[2 * k], f[2 * k + 1]);
     }
-    __device__ __forceinline__ void store(void *p, size_t i) const
+    template <bool NT = false> __device__ __forceinline__ void store(void *p, size_t i) const
     {
         typedef uint32_t V __attribute__((ext_vector_type(N / 2)));
         V x;
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) x[k] = u[k];
-        *reinterpret_cast<V *>(static_cast<uint16_t *>(p) + i) = x;
+        store_v<NT>(reinterpret_cast<V *>(static_cast<uint16_t *>(p) + i), x);
     }
     __device__ __forceinline__ void zero()
     {
@@ -46,10 +57,11 @@ template <int N> struct Raw<true, N> {
 };
 template <int N> struct Raw<false, N> {
     f32x4_t v[N / 4];
-    __device__ __forceinline__ void load(const void *p, size_t i)
+    template <bool NT = false> __device__ __forceinline__ void load(const void *p, size_t i)
     {
 #pragma unroll
-        for (int k = 0; k < N / 4; ++k) v[k] = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(p) + i + 4 * k);
+        for (int k = 0; k < N / 4; ++k)
+            v[k] = load_v<NT>(reinterpret_cast<const f32x4_t *>(static_cast<const float *>(p) + i + 4 * k));
     }
     __device__ __forceinline__ float at(int k) const { return v[k >> 2][k & 3]; }
     __device__ __forceinline__ void set(const float (&f)[N])
@@ -57,10 +69,10 @@ template <int N> struct Raw<false, N> {
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k >> 2][k & 3] = f[k];
     }
-    __device__ __forceinline__ void store(void *p, size_t i) const
+    template <bool NT = false> __device__ __forceinline__ void store(void *p, size_t i) const
     {
 #pragma unroll
-        for (int k = 0; k < N / 4; ++k) *reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + i + 4 * k) = v[k];
+        for (int k = 0; k < N / 4; ++k) store_v<NT>(reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + i + 4 * k), v[k]);
     }
     __device__ __forceinline__ void zero()
     {
@@ -69,18 +81,18 @@ template <int N> struct Raw<false, N> {
     }
     __device__ __forceinline__ void forget() {}
 };
-template <bool BF16, int N> __device__ __forceinline__ void load_n(const void *p, size_t i, float (&f)[N])
+template <bool BF16, int N, bool NT = false> __device__ __forceinline__ void load_n(const void *p, size_t i, float (&f)[N])
 {
     Raw<BF16, N> r;
-    r.load(p, i);
+    r.template load<NT>(p, i);
 #pragma unroll
     for (int k = 0; k < N; ++k) f[k] = r.at(k);
 }
-template <bool BF16, int N> __device__ __forceinline__ void store_n(void *p, size_t i, const float (&f)[N])
+template <bool BF16, bool NT = false, int N> __device__ __forceinline__ void store_n(void *p, size_t i, const float (&f)[N])
 {
     Raw<BF16, N> r;
     r.set(f);
-    r.store(p, i);
+    r.template store<NT>(p, i);
 }
 // x rounded to the stored type and back.
 template <bool BF16> __device__ __forceinline__ float as_stored(float x)
@@ -159,10 +171,10 @@ __device__ __forceinline__ uint32_t e4m3_encode4(float a, float b, float c, floa
     d = __builtin_amdgcn_fmed3f(d, ld, 448.0f);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
-__device__ __forceinline__ void e4m3_decode8(const u32x2_t &c, float (&x)[8])
+template <int N> __device__ __forceinline__ void e4m3_decode(const uint32_t (&c)[N / 4], float (&x)[N])
 {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < N / 4; ++k) {
         const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[k], false);
         const f32x2_t hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[k], true);
         x[4 * k] = lo[0];

@@ -9,6 +9,7 @@ stream are passed through ctypes.  All arithmetic runs in the HIP kernels of
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import re
 import threading
@@ -527,6 +528,7 @@ def forge_rmsnorm(x, w, *, residual=None, h=None, y=None, q=None, q_scale=None, 
             _adr(q_scale), T, d, _float_code(s, "the stream"), _float_code(w, "w"), group, eps)
 
 
+@functools.lru_cache(maxsize=256)
 def forge_rmsnorm_backward_workspace(T, d):
     """Bytes of the workspace of ``forge_rmsnorm_backward`` on [T, d]."""
     return _ops().forge_rmsnorm_backward_workspace(int(T), int(d))
@@ -585,6 +587,7 @@ class TensorList:
         _check(L.forge_tensor_list_build(arr, n, host.data_ptr(), host.nbytes, ctypes.byref(self.list)), "TensorList")
         self.table = host.to(self.device) if n else None
         self._ref = ctypes.byref(self.list)
+        self._norm_ws = L.forge_grad_norm_workspace(self._ref)
         # the table belongs to the stream that is current here (the copy itself has ended)
         self._home = torch.cuda.current_stream(self.device).cuda_stream if n else 0
 
@@ -633,7 +636,7 @@ class TensorList:
 
 def forge_grad_norm_workspace(tensors):
     """Bytes of the workspace of ``forge_grad_norm`` on a TensorList."""
-    return _ops().forge_grad_norm_workspace(tensors._ref)
+    return tensors._norm_ws
 
 
 def forge_grad_norm(tensors, out, *, max_norm, ws, stream=None):
