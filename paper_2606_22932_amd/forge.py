@@ -449,16 +449,12 @@ def _adr(t):
 
 def _float_code(t, what):
     import torch
-    if t.dtype == torch.bfloat16:
+    dt = t.dtype
+    if dt is torch.bfloat16:
         return FORGE_DTYPE_BF16
-    if t.dtype == torch.float32:
+    if dt is torch.float32:
         return FORGE_DTYPE_F32
-    raise TypeError(f"{what} must be bfloat16 or float32, got {t.dtype}")
-
-
-def _like(t, what, shape, dtype):
-    if t is not None and (t.shape != shape or t.dtype is not dtype):
-        raise ValueError(f"{what} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    raise TypeError(f"{what} must be bfloat16 or float32, got {dt}")
 
 
 def _bytes_ws(ws, need):
@@ -471,17 +467,23 @@ def _bytes_ws(ws, need):
     return ws.nbytes
 
 
-def _one_device(*ts):
-    """Index of the HIP device that all the tensors given live on, contiguous."""
+def _one_device(*specs):
+    """Index of the HIP device that the tensors of (tensor or None, name, shape, dtype) live on,
+    contiguous and as said (a shape or dtype of None: any).  One loop, for the calls on a single
+    token, which take as long as their binding."""
     dev = None
-    for t in ts:
-        if t is not None:
-            at = t.get_device()
-            if at != dev or not t.is_contiguous():
-                _dev(t)
-                if dev is not None:
-                    raise ValueError(f"tensors on different devices: {dev} and {at}")
-                dev = at
+    for t, what, shape, dtype in specs:
+        if t is None:
+            continue
+        at = t.get_device()
+        if at != dev or not t.is_contiguous():
+            _dev(t)
+            if dev is not None:
+                raise ValueError(f"tensors on different devices: {dev} and {at}")
+            dev = at
+        if (shape is not None and t.shape != shape) or (dtype is not None and t.dtype is not dtype):
+            raise ValueError(f"{what} must be {dtype or 'a tensor'} {'' if shape is None else tuple(shape)}, "
+                             f"got {t.dtype} {tuple(t.shape)}")
     return dev
 
 
@@ -509,21 +511,16 @@ def forge_rmsnorm(x, w, *, residual=None, h=None, y=None, q=None, q_scale=None, 
     [T, ceil(d / 128)] (per 128 columns).  ``h`` goes with a residual and may be the residual.
     """
     import torch
+    bf16 = torch.bfloat16
     shape = T, d = x.shape
-    dev = _one_device(x, w, residual, h, y, q, q_scale)
-    _like(w, "w", (d,), w.dtype)
-    s = x
-    if residual is not None:
-        s = residual
-        _like(x, "x beside a residual", shape, torch.bfloat16)
-        _like(residual, "residual", shape, residual.dtype)
-    _like(h, "h", shape, s.dtype)
-    _like(y, "y", shape, torch.bfloat16)
-    _like(q, "q", shape, torch.float8_e4m3fn)
-    group = 0
+    s = x if residual is None else residual
+    group, scales = 0, None
     if q is not None and q_scale is not None:
         group = FORGE_Q_GROUP if q_scale.dim() == 2 else 0
-        _like(q_scale, "q_scale", (T, (d + 127) // 128) if group else (T,), torch.float32)
+        scales = (T, (d + 127) // 128) if group else (T,)
+    dev = _one_device((x, "x beside a residual", shape, None if residual is None else bf16), (w, "w", (d,), None),
+                      (residual, "residual", shape, None), (h, "h", shape, s.dtype), (y, "y", shape, bf16),
+                      (q, "q", shape, torch.float8_e4m3fn), (q_scale, "q_scale", scales, torch.float32))
     _launch("forge_rmsnorm", dev, stream, x.data_ptr(), _adr(residual), w.data_ptr(), _adr(h), _adr(y), _adr(q),
             _adr(q_scale), T, d, _float_code(s, "the stream"), _float_code(w, "w"), group, eps)
 
@@ -539,15 +536,12 @@ def forge_rmsnorm_backward(dy, h, w, *, dres=None, dh=None, dx=None, dw, eps, ws
     dres + the norm's gradient, and dw (float32).  ``h`` is what the norm was taken of; dh may be
     dres.  ``ws``: any tensor of at least ``forge_rmsnorm_backward_workspace(T, d)`` bytes."""
     import torch
+    bf16 = torch.bfloat16
     shape = T, d = dy.shape
-    dev = _one_device(dy, h, w, dres, dh, dx, dw, ws)
-    _like(dy, "dy", shape, torch.bfloat16)
-    _like(h, "h", shape, h.dtype)
-    _like(w, "w", (d,), w.dtype)
-    _like(dres, "dres", shape, h.dtype)
-    _like(dh, "dh", shape, h.dtype)
-    _like(dx, "dx", shape, torch.bfloat16)
-    _like(dw, "dw", (d,), torch.float32)
+    ht = h.dtype
+    dev = _one_device((dy, "dy", shape, bf16), (h, "h", shape, None), (w, "w", (d,), None), (dres, "dres", shape, ht),
+                      (dh, "dh", shape, ht), (dx, "dx", shape, bf16), (dw, "dw", (d,), torch.float32),
+                      (ws, "ws", None, None))
     n = _bytes_ws(ws, forge_rmsnorm_backward_workspace(T, d))
     _launch("forge_rmsnorm_backward", dev, stream, dy.data_ptr(), h.data_ptr(), w.data_ptr(), _adr(dres), _adr(dh),
             _adr(dx), dw.data_ptr(), T, d, _float_code(h, "h"), _float_code(w, "w"), eps, _adr(ws), n)
@@ -571,6 +565,8 @@ class TensorList:
         import torch
         self.tensors = [tuple(x) + (None,) * (6 - len(x)) for x in tensors]
         n = len(self.tensors)
+        if n and torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("a TensorList is built (and its table copied to the device) outside of graph capture")
         each = lambda x: [float(x)] * n if isinstance(x, (int, float)) else [float(y) for y in x]
         self.lr_scale, self.weight_decay = each(lr_scale), each(weight_decay)
         if len(self.lr_scale) != n or len(self.weight_decay) != n:
@@ -643,8 +639,7 @@ def forge_grad_norm(tensors, out, *, max_norm, ws, stream=None):
     """out[0] = the 2-norm of all gradients of a TensorList, out[1] = min(1, max_norm / (out[0] +
     1e-6)); ``out`` float32 [2], ``out[1:]`` is what ``forge_adamw_multi`` takes as grad_scale."""
     import torch
-    dev = _one_device(out, ws, tensors.table)
-    _like(out, "out", (2,), torch.float32)
+    dev = _one_device((out, "out", (2,), torch.float32), (ws, "ws", None, None), (tensors.table, "table", None, None))
     n = _bytes_ws(ws, forge_grad_norm_workspace(tensors))
     _launch("forge_grad_norm", dev, stream if tensors.table is None else tensors._use(stream), tensors._ref,
             _adr(tensors.table), max_norm, out.data_ptr(), _adr(ws), n)
@@ -657,8 +652,8 @@ def forge_adamw_multi(tensors, *, lr, beta1, beta2, eps, step, grad_scale=None, 
     import torch
     if tensors.table is None:
         return
-    dev = _one_device(tensors.table, grad_scale)
-    if grad_scale is not None and (grad_scale.dtype is not torch.float32 or grad_scale.numel() != 1):
+    dev = _one_device((tensors.table, "table", None, None), (grad_scale, "grad_scale", None, torch.float32))
+    if grad_scale is not None and grad_scale.numel() != 1:
         raise ValueError("grad_scale must be one float32")
     _launch("forge_adamw_multi", dev, tensors._use(stream), tensors._ref, tensors.table.data_ptr(), lr, beta1, beta2,
             eps, _adr(grad_scale), int(step))

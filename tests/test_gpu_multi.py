@@ -361,6 +361,19 @@ def test_on_another_stream_and_with_new_gradients():
         assert torch.equal(a.dev[k].view(torch.uint8), b.dev[k].view(torch.uint8)), k
 
 
+def test_no_list_is_built_under_capture():
+    t = [torch.zeros(64, device="cuda") for _ in range(4)]
+    x = torch.zeros(8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.add_(1.0)
+        with pytest.raises(RuntimeError, match="outside of graph capture"):
+            forge.TensorList([t])
+    graph.replay()                                       # the capture itself goes on
+    torch.cuda.synchronize()
+    assert float(x.sum()) == 8.0
+
+
 def test_large_offsets():
     """A tensor of more than 2^30 elements: its last elements are stepped, and normed."""
     n = (1 << 30) + 4099

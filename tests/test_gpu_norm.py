@@ -100,7 +100,7 @@ def test_forward(T, d, h, w, res, group):
     check_forward(o, x, g, r, group=group)
 
 
-@pytest.mark.parametrize("T,d", [(70000, 8), (5001, 256), (1031, 1032), (515, 4096)], ids=str)
+@pytest.mark.parametrize("T,d", [(70000, 8), (5001, 256), (17001, 520), (8300, 1032), (515, 4096)], ids=str)
 @pytest.mark.parametrize("h", ["bf16", "f32"])
 def test_forward_many_rows(T, d, h):
     _say("rmsnorm rows", T, d, h)
@@ -206,7 +206,7 @@ def test_backward(T, d, h, w, res, out):
     check_backward(backward(dy, x, g, dres, out=out), dy, x, g, dres)
 
 
-@pytest.mark.parametrize("T,d", [(70000, 8), (30011, 64), (5001, 256), (1031, 1032), (515, 4096), (300, 8200)], ids=str)
+@pytest.mark.parametrize("T,d", [(70000, 8), (30011, 64), (5001, 256), (1031, 1032), (6001, 1032), (515, 4096), (300, 8200)], ids=str)
 @pytest.mark.parametrize("h", ["bf16", "f32"])
 def test_backward_many_rows(T, d, h):
     _say("rmsnorm_backward rows", T, d, h)
@@ -269,6 +269,29 @@ def test_gradient_against_differences():
         size = float((R.f64(o["dh"]) * u).abs().sum()), float((R.f64(o["dw"]) * v).abs().sum())
         assert abs(float((R.f64(o["dh"]) * u).sum()) - dif_h) < 1e-6 * size[0]
         assert abs(float((R.f64(o["dw"]) * v).sum()) - dif_w) < 1e-6 * size[1]
+
+
+def test_offsets_past_32_bits():
+    """Close to 2^31 elements of fp32: the first and the last rows of both passes."""
+    d = 4096
+    T = (1 << 31) // d - 1
+    h, w = torch.zeros((T, d), device="cuda"), rand((d,), 0.1, DT["f32"], 3, 1.0)
+    ends = [0, 1, T - 2, T - 1]
+    rows = rand((4, d), 1.2, DT["f32"], 1)
+    h[ends] = rows.cuda()
+    y = torch.zeros((T, d), dtype=torch.bfloat16, device="cuda")
+    forge.forge_rmsnorm(h, w.cuda(), y=y, eps=EPS)
+    check_forward({"y": y[ends].cpu()}, rows, w)
+    assert not y[2:T - 2].any()
+    dy = y.zero_()
+    g = rand((4, d), 1e-2, DT["bf16"], 2)
+    dy[ends] = g.cuda()
+    dw = torch.empty(d, device="cuda")
+    ws = torch.empty(forge.forge_rmsnorm_backward_workspace(T, d), dtype=torch.uint8, device="cuda")
+    dx = torch.ones((T, d), dtype=torch.bfloat16, device="cuda")
+    forge.forge_rmsnorm_backward(dy, h, w.cuda(), dx=dx, dw=dw, eps=EPS, ws=ws)
+    check_backward({"dx": dx[ends].cpu(), "dw": dw.cpu()}, g, rows, w)
+    assert not dx[2:T - 2].any()
 
 
 # ----------------------------------------------------------------------------- streams, graphs, refusals
