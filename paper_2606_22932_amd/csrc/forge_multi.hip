@@ -1,5 +1,10 @@
 // forge_multi.hip -- one pass over the tensors of a list: the norm of their gradients, and
 // their AdamW step (include/forge_ops.h).
+//
+// Both are bound by HBM.  The tensors are cut into chunks of MT_CHUNK elements; a table in device
+// memory says which tensor a chunk belongs to and what that is of, so that tensors of any sizes
+// and types take one launch, whose parallelism does not depend on how the elements are spread
+// over them.  A workgroup finds its tensor by two scalar loads one after the other.
 #include "forge_ops_device.h"
 #include "forge_ops_internal.h"
 
@@ -12,8 +17,9 @@ static_assert(MT_CHUNK == NTH * 8, "a thread's share of a chunk is eight element
 
 // A thread's share of a chunk is 8 / V vectors of V elements, the vectors of the chunk dealt out
 // in turn, so that each access of a wave is one dense run: V is 8 where nothing is wider than
-// bf16, else 4.  (fp32 in runs of eight elements a lane: every access touches half of twice the
-// lines, 1185 against 1053 us with fp32 throughout on a layer's 218 M elements.)
+// bf16, else 4.  (With fp32 in runs of eight elements a lane, every access touches half of twice the
+// lines: 1185 against 1084 us with fp32 throughout on 218 M elements, 150 against 131 us for their
+// norm.)
 
 // Elements i .. i + V - 1, of which the first n exist (n >= V: all of them); zeros after them.
 template <int TY, int V> __device__ __forceinline__ void load_some(const void *p, size_t i, int n, float (&f)[V])
@@ -26,8 +32,8 @@ template <int TY, int V> __device__ __forceinline__ void load_some(const void *p
     for (int k = 0; k < V; ++k) {
         f[k] = 0.0f;
         if (k < n) {
-            if constexpr (TY == MT_BF16) f[k] = bf_lo(static_cast<const uint16_t *>(p)[i + k]);
-            else f[k] = static_cast<const float *>(p)[i + k];
+            if constexpr (TY == MT_BF16) f[k] = bf_lo(*global_of<uint16_t>(p, i + k));
+            else f[k] = *global_of<float>(p, i + k);
         }
     }
 }
@@ -40,17 +46,16 @@ template <int TY, int V> __device__ __forceinline__ void store_some(void *p, siz
 #pragma unroll
     for (int k = 0; k < V; ++k)
         if (k < n) {
-            if constexpr (TY == MT_BF16) static_cast<uint16_t *>(p)[i + k] = (uint16_t)pack_bf16(f[k], 0.0f);
-            else static_cast<float *>(p)[i + k] = f[k];
+            if constexpr (TY == MT_BF16) *global_of<uint16_t>(p, i + k) = (uint16_t)pack_bf16(f[k], 0.0f);
+            else *global_of<float>(p, i + k) = f[k];
         }
 }
 template <int V> __device__ __forceinline__ void load_codes(const void *p, size_t i, int n, float (&f)[V])
 {
-    const uint8_t *b = static_cast<const uint8_t *>(p) + i;
     uint32_t c[V / 4];
     if (n >= V) {
         typedef uint32_t W __attribute__((ext_vector_type(V / 4)));
-        const W x = ld_nt<W>(b);
+        const W x = load_v<W, uint8_t, true>(p, i);
 #pragma unroll
         for (int k = 0; k < V / 4; ++k) c[k] = x[k];
     } else {
@@ -58,23 +63,22 @@ template <int V> __device__ __forceinline__ void load_codes(const void *p, size_
         for (int k = 0; k < V / 4; ++k) c[k] = 0;
 #pragma unroll
         for (int k = 0; k < V; ++k)
-            if (k < n) c[k >> 2] |= (uint32_t)b[k] << (8 * (k & 3));
+            if (k < n) c[k >> 2] |= (uint32_t)*global_of<uint8_t>(p, i + k) << (8 * (k & 3));
     }
     e4m3_decode<V>(c, f);
 }
 template <int V> __device__ __forceinline__ void store_codes(void *p, size_t i, int n, const uint32_t (&c)[V / 4])
 {
-    uint8_t *b = static_cast<uint8_t *>(p) + i;
     if (n >= V) {
         typedef uint32_t W __attribute__((ext_vector_type(V / 4)));
         W x;
 #pragma unroll
         for (int k = 0; k < V / 4; ++k) x[k] = c[k];
-        st_nt(b, x);
+        store_v<uint8_t, true>(p, i, x);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k)
-            if (k < n) b[k] = (uint8_t)(c[k >> 2] >> (8 * (k & 3)));
+            if (k < n) *global_of<uint8_t>(p, i + k) = (uint8_t)(c[k >> 2] >> (8 * (k & 3)));
     }
 }
 
@@ -150,8 +154,8 @@ __device__ __forceinline__ void adamw_chunk(const MtTensor &t, size_t base, cons
         if constexpr (ST == MT_FP8) {
             load_codes(t.m, at[j], n[j], m[j]);
             load_codes(t.v, at[j], n[j], v[j]);
-            ms[j] = n[j] ? t.ms[at[j] / MT_BLOCK] : 0.0f;
-            vs[j] = n[j] ? t.vs[at[j] / MT_BLOCK] : 0.0f;
+            ms[j] = n[j] ? *global_of<float>((const void *)t.ms, at[j] / MT_BLOCK) : 0.0f;
+            vs[j] = n[j] ? *global_of<float>((const void *)t.vs, at[j] / MT_BLOCK) : 0.0f;
         } else {
             load_some<ST>(t.m, at[j], n[j], m[j]);
             load_some<ST>(t.v, at[j], n[j], v[j]);
@@ -179,8 +183,8 @@ __device__ __forceinline__ void adamw_chunk(const MtTensor &t, size_t base, cons
             const float ms1 = e4m3_scale(lanes_max(mag_n(m[j]), MT_BLOCK / V));
             const float vs1 = e4m3_scale(lanes_max(mag_n(root), MT_BLOCK / V));
             if (n[j] && at[j] % MT_BLOCK == 0) {
-                t.ms[at[j] / MT_BLOCK] = ms1;
-                t.vs[at[j] / MT_BLOCK] = vs1;
+                *global_of<float>((void *)t.ms, at[j] / MT_BLOCK) = ms1;
+                *global_of<float>((void *)t.vs, at[j] / MT_BLOCK) = vs1;
             }
             const float mi = refined_inverse(ms1), vi = refined_inverse(vs1);
             float lm[V], lv[V];
@@ -214,7 +218,12 @@ __device__ __forceinline__ void adamw_state(const MtTensor &t, size_t base, cons
     else adamw_chunk<WT, GT, MT_FP8>(t, base, h, scale);
 }
 
-// One workgroup a chunk; what its tensor is of is the same for all of its threads.
+// One workgroup a chunk; what its tensor is of is the same for all of its threads.  The streams
+// are non-temporal: 1202 against 1302 us on 525 M elements with bf16 throughout.  Measured
+// (replayed from a graph): that 1205 us (6.1 TB/s; HBM counters 4.22 GB read and 3.15 written, the
+// algorithm's own), 218 M bf16 with fp8 state 370 us (6.0 TB/s; 40 vector instructions an
+// element and wave, issued in half the time), with fp32 throughout 1070 us (5.7 TB/s); 65
+// tensors of 4096 in fp32 3.0 us, which is launch and latency.
 __global__ void __launch_bounds__(NTH) adamw_multi_kernel(MtTable tab, MtHyper h, const float *grad_scale)
 {
     const int c = blockIdx.x;
@@ -274,22 +283,20 @@ struct GradShare {
         r[0] = r[1] = u32x4_t{0, 0, 0, 0};
         if (g.bf16) {
             const int at = 8 * threadIdx.x;
-            const uint16_t *p = static_cast<const uint16_t *>(g.p) + at;
-            if (at + 8 <= g.n) r[0] = *reinterpret_cast<const u32x4_t *>(p);
+            if (at + 8 <= g.n) r[0] = load_v<u32x4_t, uint16_t, false>(g.p, at);
             else
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    if (at + k < g.n) r[0][k >> 1] |= (uint32_t)p[k] << (16 * (k & 1));
+                    if (at + k < g.n) r[0][k >> 1] |= (uint32_t)*global_of<uint16_t>(g.p, at + k) << (16 * (k & 1));
         } else {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int at = 4 * (j * NTH + (int)threadIdx.x);
-                const uint32_t *p = static_cast<const uint32_t *>(g.p) + at;
-                if (at + 4 <= g.n) r[j] = *reinterpret_cast<const u32x4_t *>(p);
+                if (at + 4 <= g.n) r[j] = load_v<u32x4_t, uint32_t, false>(g.p, at);
                 else
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        if (at + k < g.n) r[j][k] = p[k];
+                        if (at + k < g.n) r[j][k] = *global_of<uint32_t>(g.p, at + k);
             }
         }
     }
@@ -313,8 +320,13 @@ struct GradShare {
     }
 };
 
-// The squares of the chunks from blockIdx.x on, gridDim.x apart.  The next chunk is looked up in
-// the table while this one's loads are in flight.
+// The squares of the chunks from blockIdx.x on, gridDim.x apart: neighbouring workgroups read
+// neighbouring chunks (a run of 52 chunks for each: 97 against 84 us on 218 M bf16).  The next
+// chunk is looked up in the table while this one's loads are in flight (80 us).  The loads are
+// plain, although non-temporal ones take 5 % less alone: the step that follows reads the
+// gradients again, and what the caches keep of them counts for more (norm and step on 100 M bf16
+// 252 against 275 us).  Measured (replayed from a graph, with the finish): 218 M bf16 80 us
+// (5.4 TB/s), fp32 150 us (5.8 TB/s), 65 tensors of 4096 in fp32 4.6 us.
 __global__ void __launch_bounds__(NTH) grad_norm_kernel(MtTable tab, double *part)
 {
     __shared__ double red[NTH / 64];

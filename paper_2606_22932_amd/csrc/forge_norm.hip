@@ -1,9 +1,13 @@
 // forge_norm.hip -- residual add and RMS norm, forward and backward (include/forge_ops.h).
 //
-// A row stays in registers between the sum of squares and the outputs, so every input is read
-// once and every output written once.  A row belongs to WR waves: one for up to 4096 columns,
-// whose reductions are lane exchanges and need no barrier; several for wider rows, which join
-// through LDS.  Narrow rows share a wave, 8, 16, 32 or 64 lanes each.
+// Both directions are bound by HBM (a few operations per element): a row stays in registers
+// between its sums and its outputs, so that every input is read once and every output written
+// once.  A row belongs to WR waves, which join their sums through LDS; rows of up to 512 columns
+// to one wave or a part of one, 8, 16 or 32 lanes, and join by lane exchanges alone.  A thread
+// holds few elements of a row (E) rather than a wave the whole of it: more waves are in flight
+// for the same registers, and a single row is spread over more loads.  One wave for up to 4096
+// columns (E = 64) measured 7.7 us at 512 x 4096 and 4.6 us at 1 x 4096, four waves of E = 16
+// 5.3 and 2.7 us; at 16384 x 4096 105 against 101 us.
 #include "forge_ops_device.h"
 #include "forge_ops_internal.h"
 
@@ -59,6 +63,16 @@ __device__ __forceinline__ void row_sum(float (&x)[N], const R &row, float (*red
     }
 }
 
+// h = round(r + x), y = h / sqrt(mean(h^2) + eps) w, and the codes of the fp32 y.
+//
+// Of the outputs only h is stored non-temporally: y and q are read by the product that follows,
+// h not before the layer's end.  A norm and a 4096 x 4096 product of its output at 2048 tokens
+// take 78 us like this, 80 with all outputs non-temporal (which alone is faster, 12.8 against
+// 15.7 us), at 8192 tokens 226 and 229.5.
+//
+// Measured (replayed from a graph): 1 x 4096 bf16 2.7 us, 512 x 4096 4.9 us, 16384 x 4096 96 us
+// (5.6 TB/s), 16384 x 8192 fp32 with fp8 output 262 us (5.65 TB/s; a large copy 4.9 to 5.4).
+// HBM counters at the latter: 808 MB read, 675 written, the algorithm's own 805 and 675.
 template <bool HB, bool WB, int E, int WR>
 __global__ void __launch_bounds__(WR == 16 ? 1024 : 256) norm_kernel(NormArgs a)
 {
@@ -161,9 +175,25 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 256) norm_kernel(NormArgs a)
     }
 }
 
+// With s = 1 / sqrt(mean(h^2) + eps): dh = dres + s (dy w - h s^2 mean(dy w h)), dw = sum of
+// dy h s over the rows.  s is formed again from h, which is read anyway.
+//
 // Each workgroup takes its rows in turn: dh and dx of each, and their share of dw in registers,
-// which it leaves in its row of the workspace.  The next rows' h and dy are loaded ahead of the
-// sums of these, so that loads are in flight across the barrier.
+// which it leaves in its row of the workspace, summed by norm_dw_kernel in an order that the
+// sizes fix.  The next rows' h and dy are loaded ahead of the sums of these, so that loads are in
+// flight across the barrier (which waits for LDS only).  dres is not: those registers would take
+// a quarter of the waves.  E = 8 with up to 16 waves a row: 91 against 110 VGPRs with E = 16, and
+// 191 against 208 us at 16384 x 8192, 105 against 108 us at 16384 x 4096.
+//
+// Inputs beyond what the L2s hold (32 MB) are read non-temporally: 94 against 104 us at 16384 x
+// 4096 and 19.0 against 20.3 us at 2048 x 4096, but 9.6 against 8.9 us at 512 x 4096.  dh and dx
+// are stored plainly for the product that follows: 4096 x 4096 products before and after this
+// kernel and it at 2048 tokens take 135 us, 142 with non-temporal stores.
+//
+// Measured (replayed from a graph, both kernels): 512 x 4096 bf16 9.5 us, of which 3.4 are
+// norm_dw_kernel; 16384 x 4096 bf16 92 us (5.8 TB/s), fp32 with dh and dx 187 us (5.7 TB/s).
+// HBM counters at 16384 x 4096 bf16: 403 MB read and 143 written, the algorithm's own 403 and 134
+// and the parts' 8.
 template <bool HB, bool NT, int E, int WR> struct GradRow {
     static constexpr int V = Row<HB, E, WR>::V, NV = Row<HB, E, WR>::NV;
     Raw<HB, V> h[NV];
@@ -188,7 +218,7 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512, 4) norm_grad_kernel(Nor
     using R = Row<HB, E, WR>;
     constexpr int V = R::V, NV = R::NV;
     __shared__ float red[2][2][16];
-    __shared__ float share[WR == 16 ? 1 : 64 * WR * E];
+    __shared__ f32x4_t share[WR == 16 ? 1 : 16 * WR * E];
     const R row(a.d);
     const float inv_d = 1.0f / a.d;
     const int stride = gridDim.x * row.slots;
@@ -259,14 +289,21 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512, 4) norm_grad_kernel(Nor
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
                     if (!row.has(j)) continue;
+                    f32x4_t *x = share + V / 4 * row.vec(j), y[V / 4];
                     if (i) {
-                        float x[V];
-                        load_n<false>(share, V * row.vec(j), x);
 #pragma unroll
-                        for (int k = 0; k < V; ++k) acc[j][k] += x[k];
+                        for (int k = 0; k < V / 4; ++k) y[k] = x[k];
+#pragma unroll
+                        for (int k = 0; k < V; ++k) acc[j][k] += y[k >> 2][k & 3];
                     }
-                    if (i + 1 < all) store_n<false>(share, V * row.vec(j), acc[j]);
-                    else store_n<false>(part, V * row.vec(j), acc[j]);
+                    if (i + 1 < all) {
+#pragma unroll
+                        for (int k = 0; k < V; ++k) y[k >> 2][k & 3] = acc[j][k];
+#pragma unroll
+                        for (int k = 0; k < V / 4; ++k) x[k] = y[k];
+                    } else {
+                        store_n<false>(part, V * row.vec(j), acc[j]);
+                    }
                 }
             }
             lds_barrier();
@@ -278,8 +315,10 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512, 4) norm_grad_kernel(Nor
     }
 }
 
-// dw: the parts' sum.  A workgroup takes 32 columns, eight threads of four columns by 32 runs of
-// parts, eight parts of a run in flight, joined through LDS in the runs' order.
+// dw: the parts' sum.  A workgroup takes 32 columns (a line of each part), eight threads of four
+// columns by 32 runs of parts, eight parts of a run in flight, joined through LDS in the runs'
+// order.  Bound by latency: 512 parts of 4096 columns 5.0 us, 256 of them 3.4; with 64 columns
+// and 16 runs to a workgroup, one part in flight each, 13.7 us.
 constexpr int DW_COLS = 32, DW_RUNS = 32;
 __global__ void __launch_bounds__(DW_RUNS * 8) norm_dw_kernel(const float *part, float *dw, int parts, int d)
 {
@@ -306,7 +345,8 @@ __global__ void __launch_bounds__(DW_RUNS * 8) norm_dw_kernel(const float *part,
     *reinterpret_cast<f32x4_t *>(dw + j) = x;
 }
 
-// Rows wider than registers hold: the row is read again (from cache) for the outputs.
+// Rows wider than registers hold: the row is read again (from cache) for the outputs, and the
+// gradient's dw is summed in the workspace.
 constexpr int NTH = 256;
 
 __device__ __forceinline__ float wide_sum(float x, float *red)

@@ -6,15 +6,29 @@
 
 namespace forge_impl {
 
-template <bool NT, class V> __device__ __forceinline__ V load_v(const V *p)
+// Device memory, told to the compiler for pointers that it cannot trace to a kernel argument (the
+// table's): it would take flat accesses for them, which occupy the LDS counter too.
+template <class T> using Global = T __attribute__((address_space(1))) *;
+template <class T> __device__ __forceinline__ Global<const T> global_of(const void *p, size_t i = 0)
 {
-    if constexpr (NT) return __builtin_nontemporal_load(p);
-    else return *p;
+    return (Global<const T>)(static_cast<const T *>(p) + i);
 }
-template <bool NT, class V> __device__ __forceinline__ void store_v(V *p, V x)
+template <class T> __device__ __forceinline__ Global<T> global_of(void *p, size_t i = 0)
 {
-    if constexpr (NT) __builtin_nontemporal_store(x, p);
-    else *p = x;
+    return (Global<T>)(static_cast<T *>(p) + i);
+}
+// Elements i .. of p as one vector V; T is what i counts.
+template <class V, class T, bool NT> __device__ __forceinline__ V load_v(const void *p, size_t i)
+{
+    const auto q = (Global<const V>)global_of<T>(p, i);
+    if constexpr (NT) return __builtin_nontemporal_load(q);
+    else return *q;
+}
+template <class T, bool NT, class V> __device__ __forceinline__ void store_v(void *p, size_t i, V x)
+{
+    const auto q = (Global<V>)global_of<T>(p, i);
+    if constexpr (NT) __builtin_nontemporal_store(x, q);
+    else *q = x;
 }
 
 // N consecutive elements (4 or 8) from p[i ..] as they lie in memory, and as fp32 values.  bf16:
@@ -25,7 +39,7 @@ template <int N> struct Raw<true, N> {
     template <bool NT = false> __device__ __forceinline__ void load(const void *p, size_t i)
     {
         typedef uint32_t V __attribute__((ext_vector_type(N / 2)));
-        const V x = load_v<NT>(reinterpret_cast<const V *>(static_cast<const uint16_t *>(p) + i));
+        const V x = load_v<V, uint16_t, NT>(p, i);
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) u[k] = x[k];
     }
@@ -41,7 +55,7 @@ template <int N> struct Raw<true, N> {
         V x;
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) x[k] = u[k];
-        store_v<NT>(reinterpret_cast<V *>(static_cast<uint16_t *>(p) + i), x);
+        store_v<uint16_t, NT>(p, i, x);
     }
     __device__ __forceinline__ void zero()
     {
@@ -61,7 +75,7 @@ template <int N> struct Raw<false, N> {
     {
 #pragma unroll
         for (int k = 0; k < N / 4; ++k)
-            v[k] = load_v<NT>(reinterpret_cast<const f32x4_t *>(static_cast<const float *>(p) + i + 4 * k));
+            v[k] = load_v<f32x4_t, float, NT>(p, i + 4 * k);
     }
     __device__ __forceinline__ float at(int k) const { return v[k >> 2][k & 3]; }
     __device__ __forceinline__ void set(const float (&f)[N])
@@ -72,7 +86,7 @@ template <int N> struct Raw<false, N> {
     template <bool NT = false> __device__ __forceinline__ void store(void *p, size_t i) const
     {
 #pragma unroll
-        for (int k = 0; k < N / 4; ++k) store_v<NT>(reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + i + 4 * k), v[k]);
+        for (int k = 0; k < N / 4; ++k) store_v<float, NT>(p, i + 4 * k, v[k]);
     }
     __device__ __forceinline__ void zero()
     {

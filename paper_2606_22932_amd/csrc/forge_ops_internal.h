@@ -42,7 +42,8 @@ hipError_t launch_rmsnorm_backward(const NormGradArgs &a, hipStream_t stream);
 
 // Columns of the widest row that the registers of a workgroup hold.
 constexpr int64_t NORM_WIDEST = 32768, GRAD_WIDEST = 16384;
-// Inputs of the gradient, in bytes, that are read non-temporally.
+// Inputs of the gradient beyond this many bytes are read non-temporally: what the L2s of eight
+// XCDs hold together.
 constexpr int64_t GRAD_CACHED = int64_t(32) << 20;
 
 // A launch over T rows: workgroups, and threads of each.
