@@ -590,26 +590,32 @@ class TensorList:
     def _entry(self, t, lr_scale, weight_decay):
         import torch
         W, G, m, v, ms, vs = t
-        _dev(*(x for x in t if x is not None))
-        if any(x is not None and x.device != self.device for x in t):
-            raise ValueError("the tensors of a list live on one device")
-        e = forge_tensor(G=G.data_ptr(), numel=G.numel(), lr_scale=lr_scale, weight_decay=weight_decay,
-                         g_dtype=_float_code(G, "gradients"))
+        at = self.device.index if self.device.type == "cuda" else -1
+        for x in t:
+            if x is not None:
+                if x.get_device() != at or at < 0:
+                    _dev(x)
+                    raise ValueError("the tensors of a list live on one device")
+                if not x.is_contiguous():
+                    _dev(x)
+        n, g = G.numel(), _float_code(G, "gradients")
         if W is None:
-            return e
-        if m is None or v is None or W.shape != G.shape or m.shape != G.shape or v.shape != G.shape:
+            return forge_tensor(None, G.data_ptr(), None, None, None, None, n, lr_scale, weight_decay, 0, g, 0, 0)
+        shape = G.shape
+        if m is None or v is None or W.shape != shape or m.shape != shape or v.shape != shape:
             raise ValueError("W, G, m and v of a tensor have one shape")
-        if m.dtype != v.dtype:
+        dt = m.dtype
+        if dt is not v.dtype:
             raise TypeError(f"m and v have one type, got {m.dtype} and {v.dtype}")
-        e.W, e.m, e.v, e.w_dtype = W.data_ptr(), m.data_ptr(), v.data_ptr(), _float_code(W, "weights")
-        if m.dtype == torch.float8_e4m3fn:
+        if dt is torch.float8_e4m3fn:
             for s in (ms, vs):
-                if s is None or s.dtype != torch.float32 or s.numel() != (G.numel() + 63) // 64:
+                if s is None or s.dtype is not torch.float32 or s.numel() != (n + 63) // 64:
                     raise ValueError("fp8 moments need float32 scales of ceil(numel / 64) elements")
-            e.m_scale, e.v_scale, e.state_dtype = ms.data_ptr(), vs.data_ptr(), FORGE_DTYPE_FP8
+            st = FORGE_DTYPE_FP8
         else:
-            e.state_dtype = _float_code(m, "moments")
-        return e
+            st, ms, vs = _float_code(m, "moments"), None, None
+        return forge_tensor(W.data_ptr(), G.data_ptr(), m.data_ptr(), v.data_ptr(), _adr(ms), _adr(vs), n, lr_scale,
+                            weight_decay, _float_code(W, "weights"), g, st, 0)
 
     def with_gradients(self, gradients):
         """A list of the same weights and state with other gradients."""
