@@ -221,8 +221,8 @@ __device__ __forceinline__ void adamw_state(const MtTensor &t, size_t base, cons
 // One workgroup a chunk; what its tensor is of is the same for all of its threads.  The streams
 // are non-temporal: 1202 against 1302 us on 525 M elements with bf16 throughout.  Measured
 // (replayed from a graph): that 1205 us (6.1 TB/s; HBM counters 4.22 GB read and 3.15 written, the
-// algorithm's own), 218 M bf16 with fp8 state 370 us (6.0 TB/s; 40 vector instructions an
-// element and wave, issued in half the time), with fp32 throughout 1070 us (5.7 TB/s); 65
+// algorithm's own), 218 M bf16 with fp8 state 370 us (6.0 TB/s; 55 vector instructions a
+// wave of elements, 300 us of the vector units' time), with fp32 throughout 1070 us (5.7 TB/s); 65
 // tensors of 4096 in fp32 3.0 us, which is launch and latency.
 __global__ void __launch_bounds__(NTH) adamw_multi_kernel(MtTable tab, MtHyper h, const float *grad_scale)
 {
