@@ -320,29 +320,42 @@ struct GradShare {
     }
 };
 
-// The squares of the chunks from blockIdx.x on, gridDim.x apart: neighbouring workgroups read
-// neighbouring chunks (a run of 52 chunks for each: 97 against 84 us on 218 M bf16).  The next
-// chunk is looked up in the table while this one's loads are in flight (80 us).  The loads are
-// plain, although non-temporal ones take 5 % less alone: the step that follows reads the
-// gradients again, and what the caches keep of them counts for more (norm and step on 100 M bf16
-// 252 against 275 us).  Measured (replayed from a graph, with the finish): 218 M bf16 80 us
-// (5.4 TB/s), fp32 150 us (5.8 TB/s), 65 tensors of 4096 in fp32 4.6 us.
-__global__ void __launch_bounds__(NTH) grad_norm_kernel(MtTable tab, double *part)
+// The squares of N neighbouring chunks at a time, from N blockIdx.x on, N gridDim.x apart:
+// neighbouring workgroups read neighbouring chunks (a run of 52 chunks for each: 97 against 84 us
+// on 218 M bf16).  The next chunks are looked up in the table while the loads of these are in
+// flight (80 us).  The loads are plain, although non-temporal ones take 5 % less alone: the step
+// that follows reads the gradients again, and what the caches keep of them counts for more (norm
+// and step on 100 M bf16 252 against 275 us).  N = 4 from 2^18 chunks on, where it leaves the
+// memory longer runs and measured faster (2 G bf16 680 against 750 us, 1 G 342 against 356, 500 M
+// 175.6 against 176.6, 1 G fp32 712 against 730); below, the fewer waves with something to read
+// cost more (100 M bf16 42.4 against 39.8, 218 M 81.3 against 79.2).  Measured (replayed from a
+// graph, with the finish): 218 M bf16 79 us (5.5 TB/s), fp32 154 us (5.7 TB/s), 65 tensors of 4096
+// in fp32 4.6 us.
+template <int N> __global__ void __launch_bounds__(NTH) grad_norm_kernel(MtTable tab, double *part)
 {
     __shared__ double red[NTH / 64];
+    const int64_t stride = (int64_t)N * gridDim.x;
     double sum = 0.0;
-    GradChunk now;
-    now.find(tab, blockIdx.x);
-    for (int64_t c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
-        GradShare g;
-        g.load(now);
-        const bool bf16 = now.bf16;
-        now.find(tab, c + gridDim.x);
-        sum = g.add_to(sum, bf16);
+    GradChunk now[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) now[k].find(tab, (int64_t)N * blockIdx.x + k);
+    for (int64_t c = (int64_t)N * blockIdx.x; c < tab.chunks; c += stride) {
+        GradShare g[N];
+        bool bf16[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            g[k].load(now[k]);
+            bf16[k] = now[k].bf16;
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) now[k].find(tab, c + stride + k);
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum = g[k].add_to(sum, bf16[k]);
     }
     sum = group_sum(sum, red);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
+constexpr int64_t NORM_LONG = int64_t(1) << 18;
 
 // The parts' sum, eight of a thread's in flight.
 __global__ void __launch_bounds__(NTH) grad_norm_finish_kernel(const double *part, int parts, float max_norm, float *out)
@@ -371,7 +384,8 @@ hipError_t launch_grad_norm(const MtTable &t, float max_norm, float *out, double
 {
     const int parts = (int)(t.chunks < MT_NORM_PARTS ? t.chunks : MT_NORM_PARTS);
     if (parts > 0) {
-        grad_norm_kernel<<<parts, NTH, 0, stream>>>(t, part);
+        if (t.chunks >= NORM_LONG) grad_norm_kernel<4><<<parts, NTH, 0, stream>>>(t, part);
+        else grad_norm_kernel<1><<<parts, NTH, 0, stream>>>(t, part);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

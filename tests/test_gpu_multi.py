@@ -288,6 +288,24 @@ def test_grad_norm_of_nothing_and_of_zeros():
         assert out.tolist() == [0.0, 1.0]
 
 
+@pytest.mark.parametrize("g", ["bf16", "f32"])
+def test_grad_norm_of_a_long_list(g):
+    """More chunks than the short lists' kernel takes: a large tensor between small ones of both
+    types, its size no multiple of four chunks; the values are set on the device."""
+    n = (1 << 18) * 2048 + 3 * 2048 + 77
+    big = torch.empty(n, dtype=DT[g], device="cuda").fill_(2.0 ** -20)
+    big[-1] = 3.0
+    small = [torch.full((5,), 2.0, device="cuda"), torch.full((3000,), 2.0 ** -10, dtype=torch.bfloat16, device="cuda")]
+    lst = forge.TensorList([(None, small[0]), (None, big), (None, small[1])])
+    assert lst.list.chunks >= 1 << 18
+    out = torch.zeros(2, device="cuda")
+    ws = torch.full((forge.forge_grad_norm_workspace(lst),), 0xFF, dtype=torch.uint8, device="cuda")
+    forge.forge_grad_norm(lst, out, max_norm=1.0, ws=ws)
+    want = ((n - 1) * 2.0 ** -40 + 9.0 + 20.0 + 3000 * 2.0 ** -20) ** 0.5      # every square is exact
+    assert abs(float(out[0].double()) - want) <= 1.01 * R.U * want
+    assert abs(float(out[1].double()) - 1 / (want + 1e-6)) <= 1.01 * R.U / want
+
+
 def test_grad_norm_of_extreme_values():
     """Squares beyond fp32's range on both sides."""
     check_norm([torch.full((1000,), 1e25), torch.full((5,), 1e-30)])
