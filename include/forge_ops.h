@@ -152,7 +152,7 @@ FORGE_API forge_status forge_tensor_list_build(const forge_tensor *tensors, int3
  * out[1] = min(1, max_norm / (out[0] + 1e-6)), the coefficient that clips them.
  *
  *   table    device copy of the list's table (may be NULL for an empty list, whose norm is 0)
- *   out      fp32 [2], output, 4-byte aligned
+ *   out      fp32 [2], output, 4-byte aligned; neither it nor ws in a tensor of the list
  *   ws       workspace of forge_grad_norm_workspace(list) bytes, 16-byte aligned, as in
  *            forge_rmsnorm_backward
  *   max_norm > 0, finite

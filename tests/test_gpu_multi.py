@@ -379,6 +379,57 @@ def test_on_another_stream_and_with_new_gradients():
         assert torch.equal(a.dev[k].view(torch.uint8), b.dev[k].view(torch.uint8)), k
 
 
+def test_a_list_of_another_stream():
+    """Built on a side stream, used on the default one (whose handle is 0) and on a third, and dropped
+    while its work is under way."""
+    a, b = (Tensor(300001, "bf16", "bf16", "bf16", seed=11) for _ in range(2))
+    torch.cuda.synchronize()
+    side, third = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        la = forge.TensorList([a.entry()])
+    forge.forge_adamw_multi(la, step=1, **HP)
+    third.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(third):
+        forge.forge_adamw_multi(la, step=2, **HP)
+    del la
+    lb = forge.TensorList([b.entry()])
+    for step in (1, 2):
+        forge.forge_adamw_multi(lb, step=step, stream=0, **HP)
+    x, y = a.after(), b.after()
+    for k in x:
+        assert torch.equal(x[k].view(torch.uint8), y[k].view(torch.uint8)), k
+
+
+def test_scalars_and_thousands_of_tensors():
+    """Tensors without an axis, and a list of 3000 whose sizes go round: each as in a list of its own."""
+    s = [torch.full((), x, device="cuda") for x in (1.0, 0.5, 0.0, 0.0)]
+    forge.forge_adamw_multi(forge.TensorList([s]), step=1, **HP)
+    z = torch.zeros(1, dtype=R.D)
+    r = R.adamw(torch.ones(1, dtype=R.D), 0.5 * torch.ones(1, dtype=R.D), z, z, step=1, **HP)
+    R.stored(s[0].cpu().view(1), r["w"], r["ew"], "scalar")
+    gen = lambda k: rand(1 + k * 37 % 4099, 0.02, k)
+    ws = [gen(k).cuda() for k in range(3000)]
+    gs = [g.mul(0.1) for g in ws]
+    st = [(torch.zeros_like(w), torch.zeros_like(w)) for w in ws]
+    forge.forge_adamw_multi(forge.TensorList([(w, g, m, v) for w, g, (m, v) in zip(ws, gs, st)]), step=1, **HP)
+    for k in range(0, 3000, 271):
+        w = gen(k)
+        z = torch.zeros(w.shape, dtype=R.D)
+        r = R.adamw(R.f64(w), R.f64(gs[k]), z, z, step=1, **HP)
+        R.stored(ws[k].cpu(), r["w"], r["ew"], f"tensor {k}")
+
+
+def test_a_gradient_shared_by_two_tensors():
+    g = rand(5000, 1e-2, 3).cuda()
+    a, b = Tensor(5000, "f32", "f32", "f32", seed=1), Tensor(5000, "f32", "f32", "bf16", seed=2)
+    for t in (a, b):
+        t.host["G"] = g.cpu()
+        t.dev["G"].copy_(g)
+    forge.forge_adamw_multi(forge.TensorList([(t.dev["W"], g, t.dev["m"], t.dev["v"]) for t in (a, b)]), step=3, **HP)
+    a.check(3)
+    b.check(3)
+
+
 def test_no_list_is_built_under_capture():
     t = [torch.zeros(64, device="cuda") for _ in range(4)]
     x = torch.zeros(8, device="cuda")
