@@ -14,7 +14,8 @@ SOURCES = [os.path.join(CSRC, f) for f in ("forge_kernels.hip", "forge_dx.hip", 
                                            "forge_norm.hip", "forge_multi.hip", "forge_api.cpp",
                                            "forge_ops_api.cpp")]
 HEADERS = [os.path.join(CSRC, f) for f in ("forge_internal.h", "forge_device.h", "forge_checks.h",
-                                           "forge_ops_internal.h", "forge_ops_device.h")]
+                                           "forge_ops_internal.h", "forge_ops_device.h",
+                                           "forge_ops_arith.h")]
 HEADERS += [os.path.join(INCLUDE, f) for f in ("forge.h", "forge_ops.h")]
 
 CEILING_SRC = os.path.join(CSRC, "hbm_ceiling.hip")

@@ -94,18 +94,6 @@ __device__ __forceinline__ float rounded_root(float x)
     const float y = z * h, root = __builtin_fmaf(__builtin_fmaf(-y, y, z), 0.5f * h, y);
     return z < __builtin_inff() ? (small ? root * 0x1p-32f : root) : z;      // Inf and NaN as they are
 }
-// x / s rounded to nearest from i = RN(1 / s): again one correction by the exact remainder (no
-// difference from IEEE division in 2.4e8 cases, i off by a step or not before its refinement).
-__device__ __forceinline__ float refined_inverse(float s)
-{
-    const float i = e4m3_inverse(s);
-    return __builtin_fmaf(__builtin_fmaf(-s, i, 1.0f), i, i);
-}
-__device__ __forceinline__ float rounded_quotient(float x, float s, float i)
-{
-    const float q = x * i;
-    return __builtin_fmaf(__builtin_fmaf(-q, s, x), i, q);
-}
 
 // One AdamW element (Algorithm 1).  fp32 and bf16 state: the arithmetic of forge_adamw's kernels
 // to the bit.  fp8 state: every operation up to the codes is one IEEE fp32 operation, none of
@@ -186,15 +174,14 @@ __device__ __forceinline__ void adamw_chunk(const MtTensor &t, size_t base, cons
                 *global_of<float>((void *)t.ms, at[j] / MT_BLOCK) = ms1;
                 *global_of<float>((void *)t.vs, at[j] / MT_BLOCK) = vs1;
             }
-            const float mi = refined_inverse(ms1), vi = refined_inverse(vs1);
             float lm[V], lv[V];
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 lm[k] = -448.0f;
                 lv[k] = root[k] > 0.0f ? 0x1p-9f : 0.0f;      // a sqrt(v) > 0 is not stored as zero
-                m[j][k] = rounded_quotient(m[j][k], ms1, mi);
-                root[k] = rounded_quotient(root[k], vs1, vi);
             }
+            e4m3_quotients(m[j], ms1);
+            e4m3_quotients(root, vs1);
             uint32_t cm[V / 4], cv[V / 4];
 #pragma unroll
             for (int k = 0; k < V / 4; ++k) {

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "forge_device.h"
+#include "forge_ops_arith.h"
 
 namespace forge_impl {
 
@@ -172,6 +173,21 @@ __device__ __forceinline__ float e4m3_scale(uint32_t amax)
 __device__ __forceinline__ float e4m3_inverse(float scale)
 {
     return scale > 0.0f ? __builtin_amdgcn_rcpf(scale) : 0.0f;
+}
+
+// The values of a block divided by its scale, as IEEE division rounds it; all zero for a scale of
+// zero, and by an Inf or NaN scale zero for every finite value.
+template <int N> __device__ __forceinline__ void e4m3_quotients(float (&x)[N], float scale)
+{
+    scale = scale < __builtin_inff() ? scale : 0.0f;
+    if (scale < E4M3_SMALL) {
+        scale *= E4M3_LIFT;
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] *= E4M3_LIFT;
+    }
+    const float i = inverse_from(scale, e4m3_inverse(scale));
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = quotient_from(x[k], scale, i);
 }
 
 // Codes of values already divided by their scale, clamped to [lo, 448] first (the hardware
