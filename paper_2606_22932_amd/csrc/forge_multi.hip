@@ -82,45 +82,64 @@ template <int V> __device__ __forceinline__ void store_codes(void *p, size_t i, 
     }
 }
 
-// sqrt(x) rounded to nearest: the product with the reciprocal root, corrected by the exact
-// remainder once.  Against the fp64 root over every fp32 mantissa, with the hardware's result and
-// its two neighbours: another value in 5 of 50331648 cases, one step off.  Small x are taken
-// times 2^64, so that no remainder underflows.
-__device__ __forceinline__ float rounded_root(float x)
+// sqrt(x) of a thread's share, rounded to nearest.  Where all lie between 2^-96 and Inf no remainder
+// needs care; else x below it is taken times 2^64, whose root is exact, and 0, Inf and NaN are their own.
+template <int V> __device__ __forceinline__ void rounded_roots(const float (&x)[V], float (&root)[V])
 {
-    const bool small = x < 0x1p-96f;
-    const float z = small ? x * 0x1p64f : x;
-    const float h = __builtin_amdgcn_rsqf(fmaxf(z, 0x1p-126f));
-    const float y = z * h, root = __builtin_fmaf(__builtin_fmaf(-y, y, z), 0.5f * h, y);
-    return z < __builtin_inff() ? (small ? root * 0x1p-32f : root) : z;      // Inf and NaN as they are
+    float lo = x[0], hi = x[0];
+#pragma unroll
+    for (int k = 1; k < V; ++k) {
+        lo = fminf(lo, x[k]);
+        hi = fmaxf(hi, x[k]);
+    }
+    if (lo >= ROOT_SMALL && hi < __builtin_inff()) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) root[k] = root_from(x[k], __builtin_amdgcn_rsqf(x[k]));
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const bool small = x[k] < ROOT_SMALL;
+        const float z = small ? x[k] * ROOT_LIFT : x[k];
+        const float y = root_from(z, __builtin_amdgcn_rsqf(z)) * (small ? ROOT_UNLIFT : 1.0f);
+        root[k] = x[k] > 0.0f && x[k] < __builtin_inff() ? y : x[k];
+    }
 }
 
-// One AdamW element (Algorithm 1).  fp32 and bf16 state: the arithmetic of forge_adamw's kernels
-// to the bit.  fp8 state: every operation up to the codes is one IEEE fp32 operation, none of
-// them fused, the root and the quotient by the scale correctly rounded.  Next to the border of
-// two codes the last bit of m' or sqrt(v') decides, and a step later that code decides a block's
-// scale; so the state of a run is what these formulas give in plain fp32 anywhere.
-template <bool EXACT>
-__device__ __forceinline__ void adamw1(float g, float &w, float &m, float &v, float &root, const MtHyper &h,
-                                       float lr_bc1, float wdf)
+__device__ __forceinline__ float adamw_weight(float w, float m, float root, const MtHyper &h, float lr_bc1, float wdf)
+{
+    const float den = __builtin_fmaf(root, h.inv_sqrt_bc2, h.eps);
+    return __builtin_fmaf(wdf, w, -((m * lr_bc1) * __builtin_amdgcn_rcpf(den)));
+}
+
+// One AdamW step of a thread's share (Algorithm 1).  fp32 and bf16 state: the arithmetic of
+// forge_adamw's kernels to the bit.  fp8 state: every operation up to the codes is one IEEE fp32
+// operation, none of them fused, the root and the quotient by the scale correctly rounded.  Next to
+// the border of two codes the last bit of m' or sqrt(v') decides, and a step later that code decides
+// a block's scale; so the state of a run is what these formulas give in plain fp32 anywhere.
+template <bool EXACT, int V>
+__device__ __forceinline__ void adamw(const float (&grad)[V], float scale, float (&w)[V], float (&m)[V], float (&v)[V],
+                                      float (&root)[V], const MtHyper &h, float lr_bc1, float wdf)
 {
     if constexpr (EXACT) {
-        m = h.b1 * m + h.c1 * g;
-        v = h.b2 * v + h.c2 * (g * g);
-        root = rounded_root(v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float g = grad[k] * scale;
+            m[k] = h.b1 * m[k] + h.c1 * g;
+            v[k] = h.b2 * v[k] + h.c2 * (g * g);
+        }
+        rounded_roots(v, root);
+#pragma unroll
+        for (int k = 0; k < V; ++k) w[k] = adamw_weight(w[k], m[k], root[k], h, lr_bc1, wdf);
     } else {
-        m = __builtin_fmaf(h.b1, m, h.c1 * g);
-        v = __builtin_fmaf(h.b2, v, (h.c2 * g) * g);
-        root = __builtin_amdgcn_sqrtf(v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float g = grad[k] * scale;
+            m[k] = __builtin_fmaf(h.b1, m[k], h.c1 * g);
+            v[k] = __builtin_fmaf(h.b2, v[k], (h.c2 * g) * g);
+            w[k] = adamw_weight(w[k], m[k], __builtin_amdgcn_sqrtf(v[k]), h, lr_bc1, wdf);
+        }
     }
-    const float den = __builtin_fmaf(root, h.inv_sqrt_bc2, h.eps);
-    w = __builtin_fmaf(wdf, w, -((m * lr_bc1) * __builtin_amdgcn_rcpf(den)));
-}
-
-// Codes of four values, of which `lo` bounds each from below.
-__device__ __forceinline__ uint32_t codes_of(const float *x, const float *lo)
-{
-    return e4m3_encode4(x[0], x[1], x[2], x[3], lo[0], lo[1], lo[2], lo[3]);
 }
 
 // A workgroup's chunk of one tensor, from element `base` on.
@@ -152,15 +171,15 @@ __device__ __forceinline__ void adamw_chunk(const MtTensor &t, size_t base, cons
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         float root[V];
+        if constexpr (ST == MT_FP8) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            if constexpr (ST == MT_FP8) {
+            for (int k = 0; k < V; ++k) {
                 m[j][k] *= ms[j];
                 v[j][k] *= vs[j];
                 v[j][k] *= v[j][k];
             }
-            adamw1<ST == MT_FP8>(g[j][k] * scale, w[j][k], m[j][k], v[j][k], root[k], h, lr_bc1, wdf);
         }
+        adamw<ST == MT_FP8>(g[j], scale, w[j], m[j], v[j], root, h, lr_bc1, wdf);
         store_some<WT>(t.W, at[j], n[j], w[j]);
         if constexpr (ST == MT_FP8) {
             if (n[j] < V) {
@@ -174,19 +193,20 @@ __device__ __forceinline__ void adamw_chunk(const MtTensor &t, size_t base, cons
                 *global_of<float>((void *)t.ms, at[j] / MT_BLOCK) = ms1;
                 *global_of<float>((void *)t.vs, at[j] / MT_BLOCK) = vs1;
             }
-            float lm[V], lv[V];
+            float above[V];
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                lm[k] = -448.0f;
-                lv[k] = root[k] > 0.0f ? 0x1p-9f : 0.0f;      // a sqrt(v) > 0 is not stored as zero
-            }
+            for (int k = 0; k < V; ++k) above[k] = root[k] * 0x1p84f;
             e4m3_quotients(m[j], ms1);
             e4m3_quotients(root, vs1);
+            // a sqrt(v) > 0 is not stored as zero: the middle of its quotient, the smallest code and
+            // 2^84 sqrt(v), which lies above both (a scale of roots is no less than 2^-84) or is zero
+#pragma unroll
+            for (int k = 0; k < V; ++k) root[k] = __builtin_amdgcn_fmed3f(root[k], 0x1p-9f, above[k]);
             uint32_t cm[V / 4], cv[V / 4];
 #pragma unroll
             for (int k = 0; k < V / 4; ++k) {
-                cm[k] = codes_of(m[j] + 4 * k, lm + 4 * k);
-                cv[k] = codes_of(root + 4 * k, lv + 4 * k);
+                cm[k] = e4m3_codes4(m[j] + 4 * k);
+                cv[k] = e4m3_codes4(root + 4 * k);
             }
             store_codes<V>(t.m, at[j], n[j], cm);
             store_codes<V>(t.v, at[j], n[j], cv);

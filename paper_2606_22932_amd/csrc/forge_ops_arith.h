@@ -5,9 +5,22 @@
 
 namespace forge_impl {
 
+// RN(sqrt(z)) from an approximation h of 1 / sqrt(z) good to two steps: root and half reciprocal
+// refined together (Goldschmidt), then the root corrected by its exact remainder (Markstein).  Right
+// for every mantissa; correcting z h alone left up to three of 2^24 a step off.  z from 2^-96 on,
+// so that no remainder underflows.
+__host__ __device__ inline float root_from(float z, float h)
+{
+    float y = z * h, k = 0.5f * h;
+    const float r = __builtin_fmaf(-k, y, 0.5f);
+    y = __builtin_fmaf(y, r, y);
+    k = __builtin_fmaf(k, r, k);
+    return __builtin_fmaf(__builtin_fmaf(-y, y, z), k, y);
+}
+
 // RN(1 / s) of a normal s from an approximation i good to two steps: two Newton steps, each from
 // the exact remainder, end at the rounded value for every mantissa but 2 - 2^-23, which is none of
-// a scale's (of no fp32 number times RN(1/448)).  Zero stays zero, for a scale of zero.
+// a scale's (of no fp32 number times RN(1/448)).
 __host__ __device__ inline float inverse_from(float s, float i)
 {
     i = __builtin_fmaf(__builtin_fmaf(-s, i, 1.0f), i, i);
@@ -23,6 +36,8 @@ __host__ __device__ inline float quotient_from(float x, float s, float i)
     return __builtin_fmaf(__builtin_fmaf(-q, s, x), i, q);
 }
 
+// Roots of values below this are taken of the value times ROOT_LIFT.
+constexpr float ROOT_SMALL = 0x1p-96f, ROOT_LIFT = 0x1p64f, ROOT_UNLIFT = 0x1p-32f;
 // Scales below this are taken times E4M3_LIFT, and their values with them, so that the remainders
 // of all that is not coded as zero are exact.
 constexpr float E4M3_SMALL = 0x1p-64f, E4M3_LIFT = 0x1p64f;

@@ -175,31 +175,35 @@ __device__ __forceinline__ float e4m3_inverse(float scale)
     return scale > 0.0f ? __builtin_amdgcn_rcpf(scale) : 0.0f;
 }
 
-// The values of a block divided by its scale, as IEEE division rounds it; all zero for a scale of
+// The values of a block divided by its scale, as IEEE division rounds them; all zero for a scale of
 // zero, and by an Inf or NaN scale zero for every finite value.
 template <int N> __device__ __forceinline__ void e4m3_quotients(float (&x)[N], float scale)
 {
-    scale = scale < __builtin_inff() ? scale : 0.0f;
-    if (scale < E4M3_SMALL) {
-        scale *= E4M3_LIFT;
+    if (!(scale >= E4M3_SMALL && scale < __builtin_inff())) {
+        const bool some = scale > 0.0f && scale < __builtin_inff();
+        const float lift = some ? E4M3_LIFT : 0.0f;
+        scale = some ? scale * E4M3_LIFT : 1.0f;
 #pragma unroll
-        for (int k = 0; k < N; ++k) x[k] *= E4M3_LIFT;
+        for (int k = 0; k < N; ++k) x[k] *= lift;
     }
-    const float i = inverse_from(scale, e4m3_inverse(scale));
+    const float i = inverse_from(scale, __builtin_amdgcn_rcpf(scale));
 #pragma unroll
     for (int k = 0; k < N; ++k) x[k] = quotient_from(x[k], scale, i);
 }
 
-// Codes of values already divided by their scale, clamped to [lo, 448] first (the hardware
-// conversion gives NaN past 464), rounded to nearest even: four to a word.
-__device__ __forceinline__ uint32_t e4m3_encode4(float a, float b, float c, float d, float la = -448.0f,
-                                                 float lb = -448.0f, float lc = -448.0f, float ld = -448.0f)
+// Codes of four values already divided by their scale, rounded to nearest even, as a word.  A
+// quotient by the scale lies at most a few steps above 448, far below 464, past which the hardware
+// conversion gives NaN.
+__device__ __forceinline__ uint32_t e4m3_codes4(const float *x)
 {
-    a = __builtin_amdgcn_fmed3f(a, la, 448.0f);
-    b = __builtin_amdgcn_fmed3f(b, lb, 448.0f);
-    c = __builtin_amdgcn_fmed3f(c, lc, 448.0f);
-    d = __builtin_amdgcn_fmed3f(d, ld, 448.0f);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false), true);
+}
+// The same, clamped to 448 first.
+__device__ __forceinline__ uint32_t e4m3_encode4(float a, float b, float c, float d)
+{
+    const float x[4] = {__builtin_amdgcn_fmed3f(a, -448.0f, 448.0f), __builtin_amdgcn_fmed3f(b, -448.0f, 448.0f),
+                        __builtin_amdgcn_fmed3f(c, -448.0f, 448.0f), __builtin_amdgcn_fmed3f(d, -448.0f, 448.0f)};
+    return e4m3_codes4(x);
 }
 template <int N> __device__ __forceinline__ void e4m3_decode(const uint32_t (&c)[N / 4], float (&x)[N])
 {
