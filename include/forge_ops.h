@@ -50,8 +50,9 @@ typedef enum {
  *   y         bf16 [T, d], output, or NULL
  *   q         fp8 E4M3 codes [T, d], output, or NULL: y = q * scale, scale = amax / 448 over
  *             a row (q_group 0; q_scale [T]) or over 128 columns, a shorter last group
- *             (q_group FORGE_Q_GROUP; q_scale [T, ceil(d / 128)]).  The codes are rounded to
- *             nearest even from the fp32 y, not from its bf16 form.  Where amax / 448 is no
+ *             (q_group FORGE_Q_GROUP; q_scale [T, ceil(d / 128)]).  The codes are the quotient
+ *             of the fp32 y, not of its bf16 form, by the scale, rounded to fp32 and from there
+ *             to nearest even; amax / 448 is the product with 1/448 rounded.  Where that is no
  *             normal number (rows of zeros among them) the scale and its codes are zero; a
  *             group that holds a NaN has a NaN scale, one that holds an Inf but no NaN an Inf
  *   q_scale   fp32, output with q

@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 256) norm_kernel(NormArgs a)
             top = max(top, mag_n(f[j]));
         }
         if (!a.q) continue;
-        float qs = 0.0f, inv = 0.0f;
+        float qs = 0.0f;
         if (a.q_group == 0) {
             top = lanes_max(top, WR == 1 ? row.lanes : 64);
             if constexpr (WR > 1) {
@@ -150,7 +150,6 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 256) norm_kernel(NormArgs a)
                 for (int i = 0; i < WR; ++i) top = max(top, redm[turn & 1][row.slot * WR + i]);
             }
             qs = e4m3_scale(top);
-            inv = e4m3_inverse(qs);
             if (live && row.lane == 0) a.qs[t] = qs;
         }
 #pragma unroll
@@ -158,18 +157,17 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 256) norm_kernel(NormArgs a)
             if (a.q_group) {
                 // 128 columns are 128 / V lanes (the launcher gives a row of up to 128 one scale)
                 qs = e4m3_scale(lanes_max(row.has(j) ? mag_n(f[j]) : 0u, 128 / V));
-                inv = e4m3_inverse(qs);
                 if (live && row.has(j) && row.vec(j) % (128 / V) == 0)
                     a.qs[(size_t)t * groups + row.vec(j) / (128 / V)] = qs;
             }
             if (!live || !row.has(j)) continue;
+            e4m3_quotients(f[j], qs);
             uint32_t *q = reinterpret_cast<uint32_t *>(a.q + at + V * row.vec(j));
             if constexpr (V == 8) {
-                const u32x2_t c = {e4m3_encode4(f[j][0] * inv, f[j][1] * inv, f[j][2] * inv, f[j][3] * inv),
-                                   e4m3_encode4(f[j][4] * inv, f[j][5] * inv, f[j][6] * inv, f[j][7] * inv)};
+                const u32x2_t c = {e4m3_codes4(f[j]), e4m3_codes4(f[j] + 4)};
                 *reinterpret_cast<u32x2_t *>(q) = c;
             } else {
-                *q = e4m3_encode4(f[j][0] * inv, f[j][1] * inv, f[j][2] * inv, f[j][3] * inv);
+                *q = e4m3_codes4(f[j]);
             }
         }
     }
@@ -395,7 +393,7 @@ __global__ void __launch_bounds__(NTH) norm_wide_kernel(NormArgs a)
 #pragma unroll
             for (int k = 0; k < 8; ++k) f[k] = f[k] * s * w[k];
         };
-        float qs = 0.0f, inv = 0.0f;
+        float qs = 0.0f;
         if (a.q && a.q_group == 0) {
             uint32_t top = 0;
             for (int v = threadIdx.x; v < nv; v += NTH) {
@@ -409,7 +407,6 @@ __global__ void __launch_bounds__(NTH) norm_wide_kernel(NormArgs a)
 #pragma unroll
             for (int k = 0; k < NTH / 64; ++k) top = max(top, redm[k]);
             qs = e4m3_scale(top);
-            inv = e4m3_inverse(qs);
             if (threadIdx.x == 0) a.qs[t] = qs;
         }
         for (int v = threadIdx.x; v < (nv + 63) / 64 * 64; v += NTH) {     // whole waves
@@ -417,14 +414,13 @@ __global__ void __launch_bounds__(NTH) norm_wide_kernel(NormArgs a)
             if (v < nv) out8(v, f);
             if (a.q && a.q_group) {
                 qs = e4m3_scale(lanes_max(mag_n(f), 16));
-                inv = e4m3_inverse(qs);
                 if (v < nv && (v & 15) == 0) a.qs[(size_t)t * groups + (v >> 4)] = qs;
             }
             if (v >= nv) continue;
             if (a.y) store_n<true>(a.y, row + 8 * v, f);
             if (a.q) {
-                const u32x2_t c = {e4m3_encode4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
-                                   e4m3_encode4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)};
+                e4m3_quotients(f, qs);
+                const u32x2_t c = {e4m3_codes4(f), e4m3_codes4(f + 4)};
                 *reinterpret_cast<u32x2_t *>(a.q + row + 8 * v) = c;
             }
         }

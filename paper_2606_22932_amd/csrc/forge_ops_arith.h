@@ -33,7 +33,7 @@ __host__ __device__ inline float inverse_from(float s, float i)
 __host__ __device__ inline float quotient_from(float x, float s, float i)
 {
     const float q = x * i;
-    return __builtin_fmaf(__builtin_fmaf(-q, s, x), i, q);
+    return __builtin_fmaf(__builtin_fmaf(q, s, -x), -i, q);      // by these signs -0 stays -0
 }
 
 // Roots of values below this are taken of the value times ROOT_LIFT.

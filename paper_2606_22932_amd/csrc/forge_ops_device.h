@@ -169,11 +169,6 @@ __device__ __forceinline__ float e4m3_scale(uint32_t amax)
     const float scale = __uint_as_float(amax) * (1.0f / 448.0f);
     return scale < 0x1p-126f ? 0.0f : scale;
 }
-// Its reciprocal to one step, zero for a scale of zero.
-__device__ __forceinline__ float e4m3_inverse(float scale)
-{
-    return scale > 0.0f ? __builtin_amdgcn_rcpf(scale) : 0.0f;
-}
 
 // The values of a block divided by its scale, as IEEE division rounds them; all zero for a scale of
 // zero, and by an Inf or NaN scale zero for every finite value.
@@ -181,10 +176,9 @@ template <int N> __device__ __forceinline__ void e4m3_quotients(float (&x)[N], f
 {
     if (!(scale >= E4M3_SMALL && scale < __builtin_inff())) {
         const bool some = scale > 0.0f && scale < __builtin_inff();
-        const float lift = some ? E4M3_LIFT : 0.0f;
         scale = some ? scale * E4M3_LIFT : 1.0f;
 #pragma unroll
-        for (int k = 0; k < N; ++k) x[k] *= lift;
+        for (int k = 0; k < N; ++k) x[k] = some ? x[k] * E4M3_LIFT : x[k] * 0.0f + 0.0f;      // no -0
     }
     const float i = inverse_from(scale, __builtin_amdgcn_rcpf(scale));
 #pragma unroll
@@ -197,13 +191,6 @@ template <int N> __device__ __forceinline__ void e4m3_quotients(float (&x)[N], f
 __device__ __forceinline__ uint32_t e4m3_codes4(const float *x)
 {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false), true);
-}
-// The same, clamped to 448 first.
-__device__ __forceinline__ uint32_t e4m3_encode4(float a, float b, float c, float d)
-{
-    const float x[4] = {__builtin_amdgcn_fmed3f(a, -448.0f, 448.0f), __builtin_amdgcn_fmed3f(b, -448.0f, 448.0f),
-                        __builtin_amdgcn_fmed3f(c, -448.0f, 448.0f), __builtin_amdgcn_fmed3f(d, -448.0f, 448.0f)};
-    return e4m3_codes4(x);
 }
 template <int N> __device__ __forceinline__ void e4m3_decode(const uint32_t (&c)[N / 4], float (&x)[N])
 {

@@ -3,7 +3,8 @@
 // steps off.  Prints how many results differ:
 //   scale      amax RN(1/448) with the mantissa 2 - 2^-23, which the inverse does not cover;
 //   inverse    1 / s, every other mantissa of s;
-//   quotient   x / s, every mantissa of s, values of x at random, next to s and at both ends;
+//   quotient   x / s, every mantissa of s, values of x at random, next to s and at both ends, and
+//              zeros of either sign;
 //   small      x / s of scales of every exponent from 2^-126 on, as a block is divided: x up to
 //              448 s, down to what is coded as zero.
 #include <cmath>
@@ -24,7 +25,8 @@ static uint32_t next(uint32_t &z) { return (z = z * 1664525u + 1013904223u) >> 9
 int main()
 {
     const uint32_t last = 0x7FFFFFu;
-    long long scales = 0, inverses = 0, quotients = 0, smalls = 0;
+    long long scales = 0, inverses = 0, smalls = 0;
+    long long quotients = !std::signbit(quotient_from(-0.0f, 3.0f, 1.0f / 3.0f)) + std::signbit(quotient_from(0.0f, 3.0f, 1.0f / 3.0f));
 #pragma omp parallel for reduction(+ : scales, inverses, quotients)
     for (uint32_t m = 0; m <= last; ++m) {
         scales += (as_bits(as_float(0x3F800000u | m) * (1.0f / 448.0f)) & last) == last;
