@@ -59,8 +59,10 @@ typedef enum {
  *   h_dtype, w_dtype  FORGE_DTYPE_F32 or FORGE_DTYPE_BF16
  *
  * At least one of y and q is given.  T >= 0; d a multiple of 8; T * d below 2^31.  T == 0 or
- * d == 0 returns FORGE_OK without a launch.  eps > 0.  The squares are summed in fp32.
- * Outputs must not overlap each other or any input, but for h == residual.
+ * d == 0 returns FORGE_OK without a launch.  eps > 0, no subnormal number.  The squares are
+ * summed in fp32: a row whose sum passes its largest number (values of about 10^17 on) has a
+ * norm of Inf and an output of zeros.  Outputs must not overlap each other or any input, but
+ * for h == residual.
  */
 FORGE_API forge_status forge_rmsnorm(const void *x, const void *residual, const void *w, void *h, void *y, void *q,
                                      float *q_scale, int64_t T, int64_t d, int32_t h_dtype, int32_t w_dtype,
@@ -177,7 +179,8 @@ FORGE_API int64_t forge_grad_norm_workspace(const forge_tensor_list *list);
  *
  *   grad_scale   device pointer to one fp32 (out + 1 of forge_grad_norm, read when the step
  *                runs), 4-byte aligned, or NULL for 1; must not lie in a weight or state tensor
- *   step, lr, beta1, beta2, eps   as in forge_adamw
+ *   step, lr, beta1, beta2, eps   as in forge_adamw, but for a subnormal eps, which is
+ *                FORGE_ERR_INVALID_HYPERPARAM here
  *
  * With fp32 or bf16 state, lr_scale 1 and no grad_scale the results are bit-identical to
  * forge_adamw's.  The weight update reads the fp32 m' and v', not their stored forms.  A

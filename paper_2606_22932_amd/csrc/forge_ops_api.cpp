@@ -2,6 +2,7 @@
 // only, before any HIP call), the per-call scalars in fp64, the layout of a tensor list, and
 // the kernel launches.
 #include <algorithm>
+#include <limits>
 #include <new>
 
 #include "forge_checks.h"
@@ -31,7 +32,9 @@ forge_status check_rows(int64_t T, int64_t d)
     return FORGE_OK;
 }
 
-bool bad_eps(float eps) { return !finite(eps) || !(eps > 0.0f); }
+// eps > 0, and no subnormal number: the hardware takes those for zero in reciprocals, and rows of
+// zeros (weights without a gradient) would become NaN.
+bool bad_eps(float eps) { return !finite(eps) || !(eps >= std::numeric_limits<float>::min()); }
 
 // One tensor of a call: what it covers and whether the call writes it.
 struct Use {
@@ -261,6 +264,7 @@ forge_status forge_adamw_multi(const forge_tensor_list *list, const void *table,
     if (list->chunks == 0) return FORGE_OK;
     if (!table || !list->steppable) return FORGE_ERR_NULL_POINTER;
     if ((s = check_hyper(lr, beta1, beta2, eps, 0.0f, step)) != FORGE_OK) return s;
+    if (bad_eps(eps)) return FORGE_ERR_INVALID_HYPERPARAM;
     if (!aligned16(table) || !aligned4(grad_scale)) return FORGE_ERR_MISALIGNED;
     if ((s = check_device()) != FORGE_OK) return s;
     const double t = static_cast<double>(step), b1 = beta1, b2 = beta2;
