@@ -11,6 +11,7 @@
 #include "forge_ops_device.h"
 #include "forge_ops_internal.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace forge_impl {
@@ -318,12 +319,18 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512, 4) norm_grad_kernel(Nor
 // order.  Bound by latency: 512 parts of 4096 columns 5.0 us, 256 of them 3.4; with 64 columns
 // and 16 runs to a workgroup, one part in flight each, 13.7 us.
 constexpr int DW_COLS = 32, DW_RUNS = 32;
-__global__ void __launch_bounds__(DW_RUNS * 8) norm_dw_kernel(const float *part, float *dw, int parts, int d)
+// Columns of one launch, which must have fewer than 2^32 threads: two rows can be 2^30 columns wide,
+// and dw of no tokens any width.
+constexpr int DW_LAUNCH = 1 << 28;
+static_assert(int64_t(DW_LAUNCH) / DW_COLS * (DW_RUNS * 8) < (int64_t(1) << 32), "threads of a launch");
+
+// Columns 0 .. cols - 1 of dw and of the parts, whose rows are d apart.
+__global__ void __launch_bounds__(DW_RUNS * 8) norm_dw_kernel(const float *part, float *dw, int parts, int d, int cols)
 {
     __shared__ f32x4_t red[DW_RUNS][8];
     const int c = threadIdx.x & 7, r = threadIdx.x >> 3, j = blockIdx.x * DW_COLS + 4 * c;
     f32x4_t x = {0, 0, 0, 0};
-    if (j < d)
+    if (j < cols)
         for (int p0 = r; p0 < parts; p0 += 8 * DW_RUNS) {
             f32x4_t y[8];
 #pragma unroll
@@ -337,7 +344,7 @@ __global__ void __launch_bounds__(DW_RUNS * 8) norm_dw_kernel(const float *part,
         }
     red[r][c] = x;
     __syncthreads();
-    if (r || j >= d) return;
+    if (r || j >= cols) return;
 #pragma unroll
     for (int k = 1; k < DW_RUNS; ++k) x += red[k][c];
     *reinterpret_cast<f32x4_t *>(dw + j) = x;
@@ -363,7 +370,7 @@ __global__ void __launch_bounds__(NTH) norm_wide_kernel(NormArgs a)
 {
     __shared__ float red[NTH / 64];
     __shared__ uint32_t redm[NTH / 64];
-    const int nv = a.d >> 3, groups = (a.d + 127) >> 7;
+    const int nv = a.d >> 3, groups = ((a.d - 1) >> 7) + 1;
     const void *src = a.r ? a.h : a.x;
     for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
         const size_t row = (size_t)t * a.d;
@@ -545,8 +552,13 @@ hipError_t launch_rmsnorm_backward(const NormGradArgs &args, hipStream_t stream)
         if (e != hipSuccess) return e;
     }
     if (parts == 1) return hipSuccess;                        // its part is dw
-    norm_dw_kernel<<<(a.d + DW_COLS - 1) / DW_COLS, DW_RUNS * 8, 0, stream>>>(a.part, a.dw, parts, a.d);
-    return hipGetLastError();
+    for (int64_t j = 0; j < a.d; j += DW_LAUNCH) {
+        const int cols = (int)std::min<int64_t>(a.d - j, DW_LAUNCH);
+        norm_dw_kernel<<<(cols + DW_COLS - 1) / DW_COLS, DW_RUNS * 8, 0, stream>>>(a.part + j, a.dw + j, parts, a.d, cols);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace forge_impl
