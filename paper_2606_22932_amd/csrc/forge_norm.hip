@@ -365,6 +365,7 @@ __device__ __forceinline__ float wide_sum(float x, float *red)
     return x;
 }
 
+// A workgroup a row.
 template <bool HB, bool WB>
 __global__ void __launch_bounds__(NTH) norm_wide_kernel(NormArgs a)
 {
@@ -372,64 +373,62 @@ __global__ void __launch_bounds__(NTH) norm_wide_kernel(NormArgs a)
     __shared__ uint32_t redm[NTH / 64];
     const int nv = a.d >> 3, groups = ((a.d - 1) >> 7) + 1;
     const void *src = a.r ? a.h : a.x;
-    for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
-        const size_t row = (size_t)t * a.d;
-        __syncthreads();                                      // red and redm are free
-        float sum = 0.0f;
+    const int t = blockIdx.x;
+    const size_t row = (size_t)t * a.d;
+    float sum = 0.0f;
+    for (int v = threadIdx.x; v < nv; v += NTH) {
+        const size_t i = row + 8 * v;
+        float f[8];
+        if (a.r) {
+            float x[8];
+            load_n<true>(a.x, i, x);
+            load_n<HB>(a.r, i, f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = as_stored<HB>(f[k] + x[k]);
+            store_n<HB>(a.h, i, f);
+        } else {
+            load_n<HB>(a.x, i, f);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum = __builtin_fmaf(f[k], f[k], sum);
+    }
+    const float s = __builtin_amdgcn_rsqf(wide_sum(sum, red) / a.d + a.eps);
+    auto out8 = [&](int v, float (&f)[8]) {
+        float w[8];
+        load_n<HB>(src, row + 8 * v, f);
+        load_n<WB>(a.w, 8 * v, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] = f[k] * s * w[k];
+    };
+    float qs = 0.0f;
+    if (a.q && a.q_group == 0) {
+        uint32_t top = 0;
         for (int v = threadIdx.x; v < nv; v += NTH) {
-            const size_t i = row + 8 * v;
             float f[8];
-            if (a.r) {
-                float x[8];
-                load_n<true>(a.x, i, x);
-                load_n<HB>(a.r, i, f);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) f[k] = as_stored<HB>(f[k] + x[k]);
-                store_n<HB>(a.h, i, f);
-            } else {
-                load_n<HB>(a.x, i, f);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum = __builtin_fmaf(f[k], f[k], sum);
+            out8(v, f);
+            top = max(top, mag_n(f));
         }
-        const float s = __builtin_amdgcn_rsqf(wide_sum(sum, red) / a.d + a.eps);
-        auto out8 = [&](int v, float (&f)[8]) {
-            float w[8];
-            load_n<HB>(src, row + 8 * v, f);
-            load_n<WB>(a.w, 8 * v, w);
+        top = lanes_max(top, 64);
+        if ((threadIdx.x & 63) == 0) redm[threadIdx.x >> 6] = top;
+        __syncthreads();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = f[k] * s * w[k];
-        };
-        float qs = 0.0f;
-        if (a.q && a.q_group == 0) {
-            uint32_t top = 0;
-            for (int v = threadIdx.x; v < nv; v += NTH) {
-                float f[8];
-                out8(v, f);
-                top = max(top, mag_n(f));
-            }
-            top = lanes_max(top, 64);
-            if ((threadIdx.x & 63) == 0) redm[threadIdx.x >> 6] = top;
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < NTH / 64; ++k) top = max(top, redm[k]);
-            qs = e4m3_scale(top);
-            if (threadIdx.x == 0) a.qs[t] = qs;
+        for (int k = 0; k < NTH / 64; ++k) top = max(top, redm[k]);
+        qs = e4m3_scale(top);
+        if (threadIdx.x == 0) a.qs[t] = qs;
+    }
+    for (int v = threadIdx.x; v < (nv + 63) / 64 * 64; v += NTH) {     // whole waves
+        float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (v < nv) out8(v, f);
+        if (a.q && a.q_group) {
+            qs = e4m3_scale(lanes_max(mag_n(f), 16));
+            if (v < nv && (v & 15) == 0) a.qs[(size_t)t * groups + (v >> 4)] = qs;
         }
-        for (int v = threadIdx.x; v < (nv + 63) / 64 * 64; v += NTH) {     // whole waves
-            float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (v < nv) out8(v, f);
-            if (a.q && a.q_group) {
-                qs = e4m3_scale(lanes_max(mag_n(f), 16));
-                if (v < nv && (v & 15) == 0) a.qs[(size_t)t * groups + (v >> 4)] = qs;
-            }
-            if (v >= nv) continue;
-            if (a.y) store_n<true>(a.y, row + 8 * v, f);
-            if (a.q) {
-                e4m3_quotients(f, qs);
-                const u32x2_t c = {e4m3_codes4(f), e4m3_codes4(f + 4)};
-                *reinterpret_cast<u32x2_t *>(a.q + row + 8 * v) = c;
-            }
+        if (v >= nv) continue;
+        if (a.y) store_n<true>(a.y, row + 8 * v, f);
+        if (a.q) {
+            e4m3_quotients(f, qs);
+            const u32x2_t c = {e4m3_codes4(f), e4m3_codes4(f + 4)};
+            *reinterpret_cast<u32x2_t *>(a.q + row + 8 * v) = c;
         }
     }
 }
@@ -505,7 +504,7 @@ template <class F> void grad_width(int64_t d, F f)
 template <bool HB, bool WB> void run_norm(const NormArgs &a, hipStream_t stream)
 {
     if (a.d > NORM_WIDEST) {
-        norm_wide_kernel<HB, WB><<<min(a.T, 1 << 20), NTH, 0, stream>>>(a);
+        norm_wide_kernel<HB, WB><<<a.T, NTH, 0, stream>>>(a);      // fewer than 2^16 rows
         return;
     }
     norm_width(a.d, [&](auto e, auto wr) {
