@@ -523,7 +523,7 @@ template <bool HB, bool WB> void run_grad(const NormGradArgs &a, int parts, hipS
     grad_width(a.d, [&](auto e, auto wr) {
         constexpr int E = decltype(e)::value, WR = decltype(wr)::value;
         const int threads = norm_grad_plan(a.T, a.d).threads;
-        if ((int64_t)a.T * a.d * (HB ? 6 : 10) > GRAD_CACHED) norm_grad_kernel<HB, WB, true, E, WR><<<parts, threads, 0, stream>>>(a);
+        if (norm_grad_streams(a.T, a.d, HB, a.dres != nullptr)) norm_grad_kernel<HB, WB, true, E, WR><<<parts, threads, 0, stream>>>(a);
         else norm_grad_kernel<HB, WB, false, E, WR><<<parts, threads, 0, stream>>>(a);
     });
 }
