@@ -116,7 +116,8 @@ typedef struct forge_tensor {
                                  sqrt(v) > 0 is never stored as zero.  All zero for a cold start.
                                  A block with a NaN has a NaN scale.  Codes and scales come from
                                  unfused, correctly rounded fp32 operations in the order of the
-                                 formulas (amax / 448 as a product with 1/448 rounded) */
+                                 formulas (amax / 448 as a product with 1/448 rounded; zero where
+                                 that is no normal number) */
     int32_t reserved;         /* 0 */
 } forge_tensor;
 

@@ -20,8 +20,7 @@ static_assert(MT_CHUNK == NTH * 8, "a thread's share of a chunk is eight element
 // A thread's share of a chunk is 8 / V vectors of V elements, the vectors of the chunk dealt out
 // in turn, so that each access of a wave is one dense run: V is 8 where nothing is wider than
 // bf16, else 4.  (With fp32 in runs of eight elements a lane, every access touches half of twice the
-// lines: 1185 against 1084 us with fp32 throughout on 218 M elements, 150 against 131 us for their
-// norm.)
+// lines: 1185 against 1084 us with fp32 throughout on 218 M elements.)
 
 // Elements i .. i + V - 1 as they lie in memory, of which the first n exist (n >= V: all of them);
 // zeros after them.
@@ -257,10 +256,10 @@ __device__ __forceinline__ void adamw_state(const MtTensor &t, size_t base, cons
 
 // One workgroup a chunk; what its tensor is of is the same for all of its threads.  The streams
 // are non-temporal: 1202 against 1302 us on 525 M elements with bf16 throughout.  Measured
-// (replayed from a graph): that 1205 us (6.1 TB/s; HBM counters 4.22 GB read and 3.15 written, the
-// algorithm's own), 218 M bf16 with fp8 state 370 us (6.0 TB/s; 55 vector instructions a
-// wave of elements, 300 us of the vector units' time), with fp32 throughout 1070 us (5.7 TB/s); 65
-// tensors of 4096 in fp32 3.0 us, which is launch and latency.
+// (replayed from a graph): that 1235 to 1270 us (5.8 to 5.95 TB/s; HBM counters 4.22 GB read and 3.15 written, the
+// algorithm's own), 218 M bf16 with fp8 state 367 us (6.1 TB/s; 51 vector instructions a
+// wave of elements, 280 us of the vector units' time), with fp32 throughout 1080 us (5.65 TB/s); 65
+// tensors of 4096 in fp32 3.2 us, which is launch and latency.
 __global__ void __launch_bounds__(NTH) adamw_multi_kernel(MtTable tab, MtHyper h, const float *grad_scale)
 {
     const int c = blockIdx.x;
@@ -366,8 +365,8 @@ struct GradShare {
 // memory longer runs and measured faster (2 G bf16 680 against 750 us, 1 G 342 against 356, 500 M
 // 175.6 against 176.6, 1 G fp32 712 against 730); below, the fewer waves with something to read
 // cost more (100 M bf16 42.4 against 39.8, 218 M 81.3 against 79.2).  Measured (replayed from a
-// graph, with the finish): 218 M bf16 79 us (5.5 TB/s), fp32 154 us (5.7 TB/s), 65 tensors of 4096
-// in fp32 4.6 us.
+// graph, with the finish): 218 M bf16 77 us (5.7 TB/s), fp32 148 us (5.9 TB/s), 65 tensors of 4096
+// in fp32 4.3 us.
 template <int N> __device__ __forceinline__ double grad_squares(const MtTable &tab)
 {
     const int64_t stride = (int64_t)N * gridDim.x;

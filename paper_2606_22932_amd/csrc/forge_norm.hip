@@ -2,12 +2,15 @@
 //
 // Both directions are bound by HBM (a few operations per element): a row stays in registers
 // between its sums and its outputs, so that every input is read once and every output written
-// once.  A row belongs to WR waves, which join their sums through LDS; rows of up to 512 columns
+// once; rows of more than 32768 columns (the gradient: 16384) are read again instead.  (The
+// gradient of an fp32 stream between 8192 and 16384 columns keeps 10 to 12 registers of 128 in
+// scratch: 4096 x 16384 184 us, 5.1 TB/s, and 107 us, 5.0 TB/s, in bf16, which spills none.)
+// A row belongs to WR waves, which join their sums through LDS; rows of up to 512 columns
 // to one wave or a part of one, 8, 16 or 32 lanes, and join by lane exchanges alone.  A thread
 // holds few elements of a row (E) rather than a wave the whole of it: more waves are in flight
 // for the same registers, and a single row is spread over more loads.  One wave for up to 4096
-// columns (E = 64) measured 7.7 us at 512 x 4096 and 4.6 us at 1 x 4096, four waves of E = 16
-// 5.3 and 2.7 us; at 16384 x 4096 105 against 101 us.
+// columns (E = 64) measured 7.7 us at 512 x 4096 and 4.3 us at 1 x 4096, four waves of E = 16
+// 4.7 and 2.4 us; at 16384 x 4096 107 against 97 us.
 #include "forge_ops_device.h"
 #include "forge_ops_internal.h"
 
@@ -71,8 +74,8 @@ __device__ __forceinline__ void row_sum(float (&x)[N], const R &row, float (*red
 // take 78 us like this, 80 with all outputs non-temporal (which alone is faster, 12.8 against
 // 15.7 us), at 8192 tokens 226 and 229.5.
 //
-// Measured (replayed from a graph): 1 x 4096 bf16 2.7 us, 512 x 4096 4.9 us, 16384 x 4096 96 us
-// (5.6 TB/s), 16384 x 8192 fp32 with fp8 output 262 us (5.65 TB/s; a large copy 4.9 to 5.4).
+// Measured (replayed from a graph): 1 x 4096 bf16 2.4 us, 512 x 4096 4.7 us, 16384 x 4096 97 us
+// (5.55 TB/s), 16384 x 8192 fp32 with fp8 output 266 us (5.6 TB/s; a large copy 4.9 to 5.4).
 // HBM counters at the latter: 808 MB read, 675 written, the algorithm's own 805 and 675.
 template <bool HB, bool WB, int E, int WR>
 __global__ void __launch_bounds__(WR == 16 ? 1024 : 256) norm_kernel(NormArgs a)
@@ -181,16 +184,19 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 256) norm_kernel(NormArgs a)
 // which it leaves in its row of the workspace, summed by norm_dw_kernel in an order that the
 // sizes fix.  The next rows' h and dy are loaded ahead of the sums of these, so that loads are in
 // flight across the barrier (which waits for LDS only).  dres is not: those registers would take
-// a quarter of the waves.  E = 8 with up to 16 waves a row: 91 against 110 VGPRs with E = 16, and
-// 191 against 208 us at 16384 x 8192, 105 against 108 us at 16384 x 4096.
+// a quarter of the waves.  E = 8 with up to 16 waves a row takes 75 VGPRs (fp32: 90),
+// E = 16 with half the waves 107 (128, and 8 to 10 spilled).  At 8192 columns E = 8 is the faster
+// (bf16, 4096 rows 54 against 55 us, 16384 rows 195 against 199), at 4096 it is not (2048 rows 20.1
+// against 18.4, 16384 rows 103 against 97).
 //
-// Inputs beyond what the L2s hold (32 MB) are read non-temporally: 94 against 104 us at 16384 x
-// 4096 and 19.0 against 20.3 us at 2048 x 4096, but 9.6 against 8.9 us at 512 x 4096.  dh and dx
+// Inputs beyond what the L2s hold (norm_grad_streams) are read non-temporally: 103 against 108 us
+// at 16384 x 4096 and 20.2 against 21.1 us at 2048 x 4096.  dh and dx
 // are stored plainly for the product that follows: 4096 x 4096 products before and after this
 // kernel and it at 2048 tokens take 135 us, 142 with non-temporal stores.
 //
-// Measured (replayed from a graph, both kernels): 512 x 4096 bf16 9.5 us, of which 3.4 are
-// norm_dw_kernel; 16384 x 4096 bf16 92 us (5.8 TB/s), fp32 with dh and dx 187 us (5.7 TB/s).
+// Measured (replayed from a graph, both kernels, on inputs that no cache holds): 512 x 4096 bf16
+// 9.7 us, of which 3.3 are norm_dw_kernel; 16384 x 4096 bf16 103 us (5.2 TB/s), fp32 with dh and dx
+// 203 us (5.3 TB/s).
 // HBM counters at 16384 x 4096 bf16: 403 MB read and 143 written, the algorithm's own 403 and 134
 // and the parts' 8.
 template <bool HB, bool NT, int E, int WR> struct GradRow {
@@ -316,7 +322,7 @@ __global__ void __launch_bounds__(WR == 16 ? 1024 : 512, 4) norm_grad_kernel(Nor
 
 // dw: the parts' sum.  A workgroup takes 32 columns (a line of each part), eight threads of four
 // columns by 32 runs of parts, eight parts of a run in flight, joined through LDS in the runs'
-// order.  Bound by latency: 512 parts of 4096 columns 5.0 us, 256 of them 3.4; with 64 columns
+// order.  Bound by latency: 512 parts of 4096 columns 4.9 us, 256 of them 3.3; with 64 columns
 // and 16 runs to a workgroup, one part in flight each, 13.7 us.
 constexpr int DW_COLS = 32, DW_RUNS = 32;
 // Columns of one launch, which must have fewer than 2^32 threads: two rows can be 2^30 columns wide,
@@ -350,8 +356,11 @@ __global__ void __launch_bounds__(DW_RUNS * 8) norm_dw_kernel(const float *part,
     *reinterpret_cast<f32x4_t *>(dw + j) = x;
 }
 
-// Rows wider than registers hold: the row is read again (from cache) for the outputs, and the
-// gradient's dw is summed in the workspace.
+// Rows wider than registers hold: the row is read again for the outputs, and once more before them
+// for the maximum of a scale per row; the gradient's dw is summed in the workspace, whose row is read
+// and written for every row but a workgroup's first.  Measured: 1024 x 65536 bf16 136 us (4.0 TB/s
+// of the bytes that it cannot do without), with fp8 output and a scale per row 130 us (3.6); the
+// gradient of 1024 x 32768 123 us (2.2), of 4096 x 32768 452 us (2.4).
 constexpr int NTH = 256;
 
 __device__ __forceinline__ float wide_sum(float x, float *red)

@@ -78,10 +78,11 @@ inline NormPlan norm_grad_plan(int64_t T, int64_t d)
     if (d > GRAD_WIDEST) return {(int)(T < 512 ? T : 512), 256};
     const int64_t waves = d <= 512 ? 1 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 4096 ? 8 : 16;   // of a row
     int64_t rows = 1;
-    // Up to four turns of one workgroup, whose sum is dw itself, take no longer than the second
-    // kernel and save its launch: 4 x 4096 bf16 4.8 against 5.2 us replayed from a graph and 8.1
-    // against 11.5 a call, 64 x 256 5.6 against 5.0 and 8.1 against 11.6 (eight turns: 8 x 4096
-    // 7.8 against 5.2, 8 x 16384 19.9 against 7.5).
+    // Up to four turns of one workgroup, whose sum is dw itself, save the second kernel and its
+    // launch: a call takes 8.1 against 11.5 us at 4 x 4096 bf16 and 8.1 against 11.6 at 64 x 256.
+    // Replayed from a graph, where launches cost less, it is 4.2 against 4.8 us at 4 x 4096 and 4.6
+    // against 4.7 at 48 x 256, but 5.2 against 4.7 at 64 x 256, four turns of rows that share a wave
+    // (eight turns: 8 x 4096 7.8 against 5.2, 8 x 16384 19.9 against 7.5).
     const bool few = T <= 4 * (waves < 8 ? 8 / waves : 1) * rows_per_wave(d);
     while (waves * rows < 8 && T > (few ? 1 : 256) * rows * rows_per_wave(d)) rows *= 2;
     const int64_t per = rows * rows_per_wave(d), n = (T + per - 1) / per;

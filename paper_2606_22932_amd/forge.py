@@ -558,7 +558,9 @@ class TensorList:
     Built once for tensors that stay where they are, and held on to while calls or captured
     graphs use it; it keeps the tensors alive.  Their types are checked and their addresses laid
     out and copied to the device here, not at each call: after gradients (or anything else) were
-    allocated anew, build another, or give the new ones to ``with_gradients``.
+    allocated anew, build another, or give the new ones to ``with_gradients``.  Either takes some
+    hundred microseconds for some hundred tensors and waits for the work queued on the current
+    stream.  A stream that calls were given by its handle outlives the list.
     """
 
     def __init__(self, tensors, *, lr_scale=1.0, weight_decay=0.0):
