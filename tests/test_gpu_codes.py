@@ -79,3 +79,38 @@ def test_state_of_a_block_with_an_infinite_value():
     keep = torch.arange(64) != 5
     assert not m[1, keep].any() and bool((m[[0, 2]] == 448).all())
     assert not torch.isfinite(m[1] * s[1]).any() and not torch.isfinite(t[3].float().cpu().view(3, 64)[1] * t[5].cpu()[1]).any()
+
+
+@pytest.mark.parametrize("w", [torch.bfloat16, F32], ids=["bf16", "f32"])
+def test_state_of_bf16_gradients_to_the_bit(w):
+    """bf16 gradients beside bf16 weights (eight elements a thread) and fp32 ones (four), over several
+    steps from cold state, with blocks of zeros, of tiny numbers and of very large ones, and a short
+    last block: codes and scales are those of plain fp32 arithmetic."""
+    n = 200035
+    gen = torch.Generator().manual_seed(17)
+    f = lambda x: torch.tensor(x, dtype=F32)
+    b1, b2 = f(0.9), f(0.999)
+    c1, c2, coef = f(1 - float(b1)), f(1 - float(b2)), f(0.37)
+    zero = lambda dt, k=n: torch.zeros(k, dtype=dt, device="cuda")
+    t = [zero(w), zero(torch.bfloat16), zero(F8), zero(F8), zero(F32, -(-n // 64)), zero(F32, -(-n // 64))]
+    lst = forge.TensorList([t])
+    pad = -n % 64
+    blocks = lambda x: torch.nn.functional.pad(x, (0, pad)).view(-1, 64)
+    q = {k: torch.zeros(n + pad).to(F8).view(-1, 64) for k in "mv"}
+    s = {k: torch.zeros(-(-n // 64)) for k in "mv"}
+    for step in range(1, 5):
+        g = (torch.randn(n, generator=gen) * 10.0 ** -step).to(torch.bfloat16)
+        g[:640], g[640:1280], g[1280:1920] = 0.0, 1e-21, 1e15
+        t[1].copy_(g)
+        forge.forge_adamw_multi(lst, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=step, grad_scale=coef.view(1).cuda())
+        x = blocks(g.float() * coef)
+        m, r = q["m"].float() * s["m"][:, None], q["v"].float() * s["v"][:, None]
+        m, v = b1 * m + c1 * x, b2 * (r * r) + c2 * (x * x)
+        root = v.double().sqrt().float()                  # the fp64 root, rounded once more, is the fp32 root
+        q["m"], s["m"] = codes_of(m)
+        code, s["v"] = codes_of(root)
+        q["v"] = torch.where(root > 0, code.float().clamp_min(2.0 ** -9), code.float()).to(F8)
+        for k, c, e in (("m", t[2], t[4]), ("v", t[3], t[5])):
+            assert torch.equal(e.cpu(), s[k]), (step, k, "scales")
+            want = q[k].view(torch.uint8).view(-1)[:n]
+            assert torch.equal(c.cpu().view(torch.uint8), want), (step, k, "codes")
